@@ -22,7 +22,8 @@
  *     device (capacity exhausted, budget too small, a bounded wait that ran out) are recorded in a
  *     status word inside the tree and returned by rt_sync_status(); nothing traps or aborts.
  *   - a tree may be used from one stream at a time; calls on one tree must not overlap on the GPU.
- *   - all arithmetic is integer; there is no floating point on this path.
+ *   - all arithmetic is integer; there is no floating point on this path (klpm_kv.h has the KV cache that the tree's
+ *     prefixes stand for, in floating point).
  */
 #ifndef KLPM_H_
 #define KLPM_H_
@@ -116,6 +117,15 @@ typedef struct { int64_t w[4]; } klpm_match_state;
 rt_status rt_match_batch_ex(rt_tree* tree, const int32_t* d_q_tokens, const int64_t* d_q_offsets, int32_t nq,
                             int32_t* d_match_len, int32_t* d_term_node, int32_t* d_term_off,
                             klpm_match_state* d_state, void* stream);
+
+/* Where the tree keeps a matched prompt: for i < nq, d_slots[i * row_stride + d] = the token-pool index of the token at depth d of
+ * query i's match, for d < min(d_match_len[i], max_len); -1 for the other d < max_len (row_stride >= max_len).  d_term_node and
+ * d_match_len are what rt_match_batch wrote; insertions since then change nothing, evictions and rt_rollback void them (the row then holds
+ * other indices of the pool, or -1).  Two prompts that share a prefix get the same indices for it, and a token keeps its index until it is
+ * evicted: with the keys and values of token-pool index s in slot s of a cache, a row is that prompt's page table with pages of one token
+ * (klpm_kv.h).  A node or length that is not one leaves a row of -1.  RT_ERR_TOO_LARGE if max_pool_tokens is above 2^31 - 1. */
+rt_status rt_prefix_slots(const rt_tree* tree, const int32_t* d_term_node, const int32_t* d_match_len, int32_t nq,
+                          int32_t* d_slots, int64_t row_stride, int32_t max_len, void* stream);
 
 /* Counters of the tree (synchronises the stream the tree was last used on).  Any pointer may be NULL.
  * n_nodes: live nodes, root excluded; n_tokens: tokens held by live nodes; clock: prompts processed;

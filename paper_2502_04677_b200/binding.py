@@ -1,6 +1,6 @@
 """ctypes binding of libklpm.so: argument marshalling only.
 
-Same names as the C ABI (include/klpm.h).  Tensors must live on the CUDA device; every step of the
+Same names as the C ABI (include/klpm.h; include/klpm_kv.h for the KV cache).  Tensors must live on the CUDA device; every step of the
 path runs in the library's kernels.  There is no CPU fallback: importing this module fails if the
 library has not been built, and every call fails on a non-CUDA tensor.
 """
@@ -57,6 +57,8 @@ _lib.rt_match_batch.restype = _i32
 _lib.rt_match_batch.argtypes = [_vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp]
 _lib.rt_match_batch_ex.restype = _i32
 _lib.rt_match_batch_ex.argtypes = [_vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp]
+_lib.rt_prefix_slots.restype = _i32
+_lib.rt_prefix_slots.argtypes = [_vp, _vp, _vp, _i32, _vp, _i64, _i32, _vp]
 _lib.rt_stats.restype = _i32
 _lib.rt_stats.argtypes = [_vp] + [ctypes.POINTER(_i64)] * 5
 _lib.rt_clone.restype = _i32
@@ -96,7 +98,7 @@ _lib.klpm_run.argtypes = [_vp, _vp, _vp, _vp, _i32, ctypes.POINTER(klpm_params),
 
 MATCH_STATE_BYTES = 32
 
-EXPORTS = ["klpm_abi_version", "rt_create", "rt_build", "rt_insert", "rt_match_batch", "rt_match_batch_ex", "rt_stats",
+EXPORTS = ["klpm_abi_version", "rt_create", "rt_build", "rt_insert", "rt_match_batch", "rt_match_batch_ex", "rt_prefix_slots", "rt_stats",
            "rt_sync_status", "rt_status_detail", "rt_clone", "rt_checkpoint", "rt_rollback", "rt_destroy", "klpm_select", "klpm_select_topk", "klpm_select_noalloc", "klpm_replay", "klpm_run", "klpm_run_ex", "klpm_run_path", "klpm_batch_times", "klpm_debug_set", "klpm_run_last_only_batch", "rt_debug_counters"]
 
 
@@ -120,6 +122,15 @@ def _stream() -> int:
     """The current stream's handle.  (Without a torch.cuda.Stream object around it: that object costs more than the
     launches of a small call.)"""
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _table(t: torch.Tensor, name: str):
+    """Pointer and row stride of a page table: int32, two dimensions, entries of a row next to one another."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor (this library has no CPU path)" % name)
+    if t.dtype is not torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be a two-dimensional int32 tensor with contiguous rows" % name)
+    return t.data_ptr(), t.stride(0)
 
 
 def _check(code: int, where: str) -> None:
@@ -202,6 +213,17 @@ def rt_match_batch_ex(tree: Tree, q_tokens: torch.Tensor, q_offsets: torch.Tenso
                                   nq, _dev(match_len, torch.int32, "match_len"), _dev(term_node, torch.int32, "term_node", True),
                                   _dev(term_off, torch.int32, "term_off", True), _dev(state, torch.int64, "state", True),
                                   _stream()), "rt_match_batch_ex")
+
+
+def rt_prefix_slots(tree: Tree, term_node: torch.Tensor, match_len: torch.Tensor, slots: torch.Tensor) -> None:
+    """slots (int32[nq, max_len]) receives the token-pool indices of every query's match, -1 behind its end: the page
+    table of the cached prefixes with pages of one token (see include/klpm.h)."""
+    nq = match_len.numel()
+    if term_node.numel() != nq or slots.dim() != 2 or slots.shape[0] != nq:
+        raise ValueError("term_node, match_len and the rows of slots must be one per query")
+    p, stride = _table(slots, "slots")
+    _check(_lib.rt_prefix_slots(tree.handle, _dev(term_node, torch.int32, "term_node"), _dev(match_len, torch.int32, "match_len"), nq,
+                                p, stride, slots.shape[1], _stream()), "rt_prefix_slots")
 
 
 def rt_stats(tree: Tree) -> dict:
@@ -372,3 +394,192 @@ def klpm_run_ex(tree: Tree, q_tokens: torch.Tensor, q_offsets: torch.Tensor, arr
                             _dev(order, torch.int32, "order"), _dev(uncached, torch.int32, "uncached"),
                             _dev(ttft, torch.int64, "ttft"), _dev(completion, torch.int64, "completion", True), _stream()),
            "klpm_run_ex")
+
+
+# ---- the KV cache behind the tree (include/klpm_kv.h) ----
+
+KV_F32, KV_BF16, KV_F16, KV_E4M3 = 0, 1, 2, 3
+KV_MAX_HEAD_DIM = 256
+_KV_TYPES = {torch.float32: KV_F32, torch.bfloat16: KV_BF16, torch.float16: KV_F16, torch.float8_e4m3fn: KV_E4M3}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+class kv_cache(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("dtype", _i32), ("n_pages", _i32), ("page_size", _i32), ("n_heads", _i32),
+                ("head_dim", _i32), ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float), ("k_stride", _i64 * 3),
+                ("v_stride", _i64 * 3)]
+
+
+class kv_rows(ctypes.Structure):
+    _fields_ = [("data", _vp), ("dtype", _i32), ("n_heads", _i32), ("stride", _i64 * 2)]
+
+
+class kv_rope(ctypes.Structure):
+    _fields_ = [("d_turns", _vp), ("rot_dim", _i32), ("interleaved", _i32), ("factor", ctypes.c_float)]
+
+
+_pc, _pr, _p2 = ctypes.POINTER(kv_cache), ctypes.POINTER(kv_rows), ctypes.POINTER(_i64)
+_f32, _f64 = ctypes.c_float, ctypes.c_double
+_lib.kv_rope_table.restype = _i32
+_lib.kv_rope_table.argtypes = [_vp, _i32, _f64, _i32, _f64, _f64, _f64, _f64, ctypes.POINTER(_f32), _vp]
+_lib.kv_rope_append.restype = _i32
+_lib.kv_rope_append.argtypes = [_pc, ctypes.POINTER(kv_rope), _vp, _vp, _i32, _pr, _pr, _pr, _pr, _vp]
+_lib.kv_decode_workspace.restype = _i64
+_lib.kv_decode_workspace.argtypes = [_pc, _i32, _i32, _i32, _i32]
+_lib.kv_decode.restype = _i32
+_lib.kv_decode.argtypes = [_pc, _pr, _pr, _i32, _vp, _i64, _i32, _vp, _f32, _i32, _vp, _vp, _p2, _vp, _i64, _vp]
+_lib.kv_evict.restype = _i32
+_lib.kv_evict.argtypes = [_pc, _vp, _p2, _i32, _vp, _i64, _i32, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _p2, _i32, _vp, _vp]
+
+KV_EXPORTS = ["kv_rope_table", "kv_rope_append", "kv_decode_workspace", "kv_decode", "kv_evict"]
+
+
+def _here(device: torch.device) -> None:
+    """The calls launch on the current device's current stream: tensors of another device are refused."""
+    if device.index != torch.cuda.current_device():
+        raise ValueError("tensors are on %s, the current device is cuda:%d" % (device, torch.cuda.current_device()))
+
+
+class KvCache:
+    """A paged KV cache: k and v are CUDA tensors [n_pages, page_size, n_heads, head_dim] (any strides, head_dim contiguous) of one
+    dtype, bfloat16, float16 or float8_e4m3fn.  An 8-bit element stands for its value times k_scale (v_scale).  The tensors are kept
+    alive by this object."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: float = 1.0, v_scale: float = 1.0):
+        if not k.is_cuda or not v.is_cuda:
+            raise ValueError("k and v must be CUDA tensors (this library has no CPU path)")
+        if k.dim() != 4 or k.shape != v.shape or k.dtype is not v.dtype or k.device != v.device:
+            raise ValueError("k and v must be [n_pages, page_size, n_heads, head_dim] tensors of one shape, dtype and device")
+        if k.dtype not in (torch.bfloat16, torch.float16, torch.float8_e4m3fn):
+            raise ValueError("a cache holds bfloat16, float16 or float8_e4m3fn")
+        if k.stride(3) != 1 or v.stride(3) != 1:
+            raise ValueError("head_dim must be contiguous")
+        self.k, self.v, self.device = k, v, k.device
+        self.n_pages, self.page_size, self.n_heads, self.head_dim = k.shape
+        if max(k.shape) >= 1 << 31:
+            raise ValueError("a dimension of the cache is too large")
+        self.c = kv_cache(k.data_ptr(), v.data_ptr(), _KV_TYPES[k.dtype], *k.shape, float(k_scale), float(v_scale),
+                          (_i64 * 3)(*k.stride()[:3]), (_i64 * 3)(*v.stride()[:3]))
+
+
+class Rope:
+    """Rotary positions as kv_rope_append takes them (made by kv_rope_table)."""
+
+    def __init__(self, turns: torch.Tensor, rot_dim: int, interleaved: bool, factor: float):
+        self.turns, self.factor = turns, factor
+        self.c = kv_rope(turns.data_ptr(), rot_dim, int(interleaved), factor)
+
+
+def kv_rope_table(rot_dim: int, theta: float = 10_000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
+                  original_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda") -> Rope:
+    """The frequencies of rotary positions over the first rot_dim elements of a head, scaled for contexts `factor` times as long as
+    original_len: scaling "none", "linear", "ntk" or "yarn" (see include/klpm_kv.h)."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError("scaling must be one of %s" % ", ".join(sorted(ROPE_SCALINGS)))
+    turns = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.float64, device=device)
+    _here(turns.device)
+    f = _f32()
+    _check(_lib.kv_rope_table(turns.data_ptr(), int(rot_dim), float(theta), ROPE_SCALINGS[scaling], float(factor), float(original_len),
+                              float(beta_fast), float(beta_slow), ctypes.byref(f), _stream()), "kv_rope_table")
+    return Rope(turns, int(rot_dim), interleaved, f.value)
+
+
+def _rows(t: torch.Tensor, cache: KvCache, n: int, name: str) -> kv_rows:
+    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != cache.head_dim or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError("%s must be [%d, heads, %d] with contiguous head_dim" % (name, n, cache.head_dim))
+    if t.device != cache.device or t.dtype not in _KV_TYPES:
+        raise ValueError("%s must be a floating-point tensor on the cache's device" % name)
+    return kv_rows(t.data_ptr(), _KV_TYPES[t.dtype], t.shape[1], (_i64 * 2)(t.stride(0), t.stride(1)))
+
+
+def _on(t: torch.Tensor, device: torch.device, name: str) -> torch.Tensor:
+    if t.device != device:
+        raise ValueError("%s must be on the cache's device" % name)
+    return t
+
+
+def kv_rope_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                   rope: Optional[Rope] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> None:
+    """Rotate q [n, q_heads, head_dim] into q_out and k by positions (int32[n]), and store k and v [n, n_heads, head_dim] at slots
+    (int32[n]) of the cache.  q_out may be q.  Without rope nothing is rotated; rows with a slot out of range are not stored."""
+    n = slots.numel()
+    _here(cache.device)
+    _on(slots, cache.device, "slots")
+    if rope is not None and (positions is None or positions.numel() != n):
+        raise ValueError("rope needs one position per row")
+    if positions is not None:
+        _on(positions, cache.device, "positions")
+    if rope is not None:
+        _on(rope.turns, cache.device, "the table of rope")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    _check(_lib.kv_rope_append(cache.c, rope.c if rope is not None else None, _dev(positions, torch.int32, "positions", True),
+                               _dev(slots, torch.int32, "slots"), n, _rows(q, cache, n, "q") if q is not None else None,
+                               _rows(q_out, cache, n, "q_out") if q is not None else None, _rows(k, cache, n, "k"),
+                               _rows(v, cache, n, "v"), _stream()), "kv_rope_append")
+
+
+def kv_decode_workspace(cache: KvCache, n_seqs: int, n_q_heads: int, max_pages: int, with_weight: bool = False) -> torch.Tensor:
+    """Device memory for the workspace of a kv_decode of these sizes.  One call uses it at a time."""
+    n = _lib.kv_decode_workspace(cache.c, int(n_seqs), int(n_q_heads), int(max_pages), int(with_weight))
+    if n < 0:
+        _check(n, "kv_decode_workspace")
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=cache.device)
+
+
+def _weight(t: torch.Tensor, cache: KvCache, n: int, least: int, name: str):
+    if t.dtype is not torch.float32 or t.dim() != 3 or t.shape[0] != n or t.shape[1] != cache.n_heads or t.shape[2] < least \
+            or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError("%s must be a float32 [%d, %d, >= %d] tensor with contiguous rows" % (name, n, cache.n_heads, least))
+    _on(t, cache.device, name)
+    return t.data_ptr(), (_i64 * 2)(t.stride(0), t.stride(1))
+
+
+def kv_decode(cache: KvCache, q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, out: torch.Tensor,
+              scale: Optional[float] = None, window: int = 0, lse: Optional[torch.Tensor] = None,
+              weight: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """Attention of one new token per sequence: q, out [n_seqs, q_heads, head_dim], page_table int32[n_seqs, max_pages], lengths
+    int32[n_seqs].  scale defaults to head_dim ** -0.5.  lse float32[n_seqs, q_heads] receives the logarithm of the softmax's sum;
+    weight float32[n_seqs, n_heads, max_pages * page_size] is increased by what every cached token received.  Without a
+    workspace (kv_decode_workspace) the call takes one from torch's allocator."""
+    n = lengths.numel()
+    _here(cache.device)
+    if page_table.dim() != 2 or page_table.shape[0] != n:
+        raise ValueError("page_table must have one row per sequence")
+    for t, name in ((page_table, "page_table"), (lengths, "lengths")):
+        _on(t, cache.device, name)
+    table, stride = _table(page_table, "page_table")
+    max_pages = page_table.shape[1]
+    if lse is not None and _on(lse, cache.device, "lse").shape != q.shape[:2]:
+        raise ValueError("lse must be [n_seqs, q_heads]")
+    w, ws = _weight(weight, cache, n, max_pages * cache.page_size, "weight") if weight is not None else (None, None)
+    if workspace is None:
+        workspace = kv_decode_workspace(cache, n, q.shape[1], max_pages, weight is not None)
+    _check(_lib.kv_decode(cache.c, _rows(q, cache, n, "q"), _rows(out, cache, n, "out"), n, table, stride, max_pages,
+                          _dev(lengths, torch.int32, "lengths"), cache.head_dim ** -0.5 if scale is None else float(scale), int(window),
+                          _dev(lse, torch.float32, "lse", True), w, ws,
+                          _dev(_on(workspace, cache.device, "workspace"), torch.uint8, "workspace"), workspace.numel(), _stream()), "kv_decode")
+
+
+def kv_evict(cache: KvCache, weight: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, new_table: torch.Tensor, keep: int,
+             sinks: int = 0, recent: int = 0, *, index: torch.Tensor, new_weight: torch.Tensor, new_lengths: torch.Tensor) -> None:
+    """Shorten every sequence to `keep` tokens per cache head: the first `sinks`, the last `recent`, then the largest weight
+    (float32[n_seqs, n_heads, >= max_pages * page_size]).  They are copied to the pages of new_table (int32[n_seqs, new_pages]), which
+    must not be pages of page_table; index int32[n_seqs, n_heads, keep], new_weight float32[n_seqs, n_heads, >= keep] and new_lengths
+    int32[n_seqs] receive which, their weights, and how many."""
+    n = lengths.numel()
+    _here(cache.device)
+    for t, name in ((page_table, "page_table"), (new_table, "new_table")):
+        if t.dim() != 2 or t.shape[0] != n:
+            raise ValueError("%s must have one row per sequence" % name)
+    for t, name in ((page_table, "page_table"), (new_table, "new_table"), (lengths, "lengths"), (index, "index"), (new_lengths, "new_lengths")):
+        _on(t, cache.device, name)
+    if new_lengths.numel() != n or tuple(index.shape) != (n, cache.n_heads, keep):
+        raise ValueError("new_lengths must be [n_seqs] and index [n_seqs, n_heads, keep]")
+    table, stride = _table(page_table, "page_table")
+    fresh, fresh_stride = _table(new_table, "new_table")
+    w, ws = _weight(weight, cache, n, page_table.shape[1] * cache.page_size, "weight")
+    nw, nws = _weight(new_weight, cache, n, keep, "new_weight")
+    _check(_lib.kv_evict(cache.c, w, ws, n, table, stride, page_table.shape[1], _dev(lengths, torch.int32, "lengths"), fresh, fresh_stride,
+                         new_table.shape[1], int(keep), int(sinks), int(recent), _dev(index, torch.int32, "index"), nw, nws,
+                         new_weight.shape[2], _dev(new_lengths, torch.int32, "new_lengths"), _stream()), "kv_evict")

@@ -7,21 +7,21 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = os.path.join(HERE, "csrc", "klpm.cu")
-HDR = os.path.join(ROOT, "include", "klpm.h")
+SRC = [os.path.join(HERE, "csrc", name) for name in ("klpm.cu", "klpm_kv.cu")]
+HDR = [os.path.join(ROOT, "include", name) for name in ("klpm.h", "klpm_kv.h")]
 LIB = os.path.join(HERE, "libklpm.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include")]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "0", "-I", os.path.join(ROOT, "include")]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    newest = max(os.path.getmtime(SRC), os.path.getmtime(HDR))
+    newest = max(os.path.getmtime(p) for p in SRC + HDR)
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= newest:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + ".%d.tmp" % os.getpid()
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + [SRC, "-o", tmp]
+    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + SRC + ["-o", tmp]
     subprocess.check_call(cmd)
     os.replace(tmp, LIB)
     return LIB

@@ -386,6 +386,29 @@ __device__ __forceinline__ int32_t walk_chain(const TreeDev& T, const int32_t* _
     }
 }
 
+// Where the tokens of a match are in the pool, one CTA per query: the edges from the node where the match ended up to the
+// root.  Bound by the chain of parents (one dependent trip per node) for few queries, by the writes for many.
+__global__ void __launch_bounds__(256) prefix_slots_kernel(const TreeDev T, const int32_t* __restrict__ tnode,
+                                                           const int32_t* __restrict__ mlen, int32_t* __restrict__ slots,
+                                                           int64_t row_stride, int32_t max_len) {
+    int32_t* row = slots + (int64_t)blockIdx.x * row_stride;
+    const int32_t m = __ldg(mlen + blockIdx.x);
+    const long long n_nodes = *reinterpret_cast<const volatile long long*>(&T.st->n_nodes);
+    int32_t v = __ldg(tnode + blockIdx.x);
+    int32_t hi = m < 0 ? 0 : m;                      // depths below hi are still to be written
+    if (v <= 0 || (long long)v >= n_nodes || hi > T.depth_start[v] + T.span_len[v]) { v = 0; hi = 0; }
+    for (int64_t d = (int64_t)hi + threadIdx.x; d < max_len; d += blockDim.x) row[d] = -1;
+    for (long long hops = 0; v > 0 && hi > 0 && hops < n_nodes; ++hops) {
+        const int32_t lo = T.depth_start[v];
+        const int64_t off = T.span_off[v] - lo;
+        const int64_t end = hi < max_len ? hi : max_len;
+        for (int64_t d = (int64_t)lo + threadIdx.x; d < end; d += blockDim.x) row[d] = (int32_t)(off + d);
+        if (lo < hi) hi = lo;
+        v = T.parent[v];
+    }
+    for (int64_t d = threadIdx.x; d < hi && d < max_len; d += blockDim.x) row[d] = -1;
+}
+
 // ------------------------------------------------------------------------------------------------
 // single-thread tree updates (callers serialise them)
 // ------------------------------------------------------------------------------------------------
@@ -6349,6 +6372,18 @@ rt_status rt_match_batch(const rt_tree* tree, const int32_t* d_q_tokens, const i
                          int32_t* d_match_len, int32_t* d_term_node, int32_t* d_term_off, void* stream) {
     return rt_match_batch_ex(const_cast<rt_tree*>(tree), d_q_tokens, d_q_offsets, nq, d_match_len, d_term_node, d_term_off,
                              nullptr, stream);
+}
+
+rt_status rt_prefix_slots(const rt_tree* tree, const int32_t* d_term_node, const int32_t* d_match_len, int32_t nq,
+                          int32_t* d_slots, int64_t row_stride, int32_t max_len, void* stream) {
+    if (!tree || nq < 0 || max_len < 0 || (nq > 0 && (!d_term_node || !d_match_len)) || (nq > 0 && max_len > 0 && !d_slots)) return RT_ERR_INVALID;
+    if (nq > 1 && row_stride < max_len) return RT_ERR_INVALID;
+    if (tree->dev.max_pool > 0x7fffffffLL) return RT_ERR_TOO_LARGE;
+    if (nq == 0 || max_len == 0) return RT_OK;
+    const_cast<rt_tree*>(tree)->last_stream = (cudaStream_t)stream;
+    prefix_slots_kernel<<<(unsigned)nq, 256, 0, (cudaStream_t)stream>>>(tree->dev, d_term_node, d_match_len, d_slots, row_stride, max_len);
+    CK(cudaGetLastError());
+    return RT_OK;
 }
 
 rt_status rt_stats(rt_tree* tree, int64_t* n_nodes, int64_t* n_tokens, int64_t* clock, int64_t* evictions, int64_t* pool_used) {
