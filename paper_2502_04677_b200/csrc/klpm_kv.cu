@@ -255,6 +255,22 @@ template <int TX, int TC> void launch_append(const AppendArgs& A, bool vec, unsi
 
 // ------------------------------------------------------------------------------------------------
 // attention of one new token
+//
+// out_h = sum_t p_t v_t / sum_t p_t with p_t = 2^(s_t - m), s_t = scale log2(e) q_h . k_t and m the largest s_t seen so far; when m
+// grows, what has been summed is multiplied by 2^(old m - new m).  Parts of a sequence are joined by the same rule.
+//
+// The floor is one read of the cache's rows (512 B per token and cache head at 128 elements of 16 bits, against a few flops per
+// byte), so everything is laid out for loads in flight:
+//   - The query heads of a cache head go through the tensor cores together (mma.sync, 16 x 8 x 16): a tile of keys is read
+//     once for all of them.  tcgen05 has nothing to give here: its tiles would hold 128 rows of heads where there are 1 to 16.
+//   - A warp works alone: its tiles (16 or 32 tokens) come through a ring of its own in shared memory (cp.async, 16 bytes a lane, 3
+//     stages of 8 KB), with its own m and sums.  No barrier in the loop.
+//   - All tiles of the batch, in the order (sequence, unit, tile), are cut into equal spans, one per warp of a grid that fills the
+//     GPU once: ragged lengths leave no warp with more than another.  A row that is cut is joined by decode_join_kernel.
+//     A unit is a cache head and up to 8 NT of its query heads.
+//   - Probabilities enter the second product as the sum of two 16-bit numbers (16 bits of precision or more).  With up to 8
+//     heads in a 16-row operand the second one takes the 8 free rows: it costs nothing.  f16 probabilities are scaled by 2^15 so that
+//     small ones keep their bits.  A bf16 query next to an 8-bit cache is split into two f16 numbers in the same way.
 // ------------------------------------------------------------------------------------------------
 struct DecodeArgs {
     CacheDev c;
@@ -262,10 +278,40 @@ struct DecodeArgs {
     const int32_t *table, *len;
     int64_t table_stride;
     int32_t n_seqs, group, max_tokens, window;
+    int32_t head_tiles, units;         // units of a cache head, of a sequence
     float scale;
-    float* lse;
-    float* weight;
+    float* lse;                        // nullable
+    float* weight;                     // nullable
     int64_t ws[2];
+    // workspace
+    long long* tiles_before;           // [n_seqs + 1] tiles of the sequences before
+    float* lse2;                       // [n_seqs, q heads] base-2 logarithm of the softmax's sum (with weight only)
+    float* part;                       // [warps][2][8 NT][2 + DP]: m, sum, output of the two rows that a warp may share with others
+    float* score;                      // [n_seqs, q heads, score_len] (with weight only)
+    int64_t score_len;
+    int32_t warps;
+};
+
+#define KLPM_DECODE_WARPS 4             // of a CTA
+#define KLPM_DECODE_MIN_SPAN 2          // tiles
+#define KLPM_SMS 148
+
+template <int TQ_, int TC_, int DP_, int NT_> struct Dec {
+    static constexpr int TQ = TQ_, TC = TC_, DP = DP_, NT = NT_;
+    static constexpr bool E8 = TC == KV_E4M3;
+    static constexpr bool HALF = E8 || TC == KV_F16;           // the products are of f16, else of bf16
+    static constexpr bool QLO = E8 && TQ == KV_BF16;           // the query is split into two f16 numbers
+    static constexpr int ROW = DP * (E8 ? 1 : 2);              // bytes of a row in shared memory
+    static constexpr int CH = ROW / 16;
+    static constexpr int TT = (E8 ? DP <= 128 : DP <= 64) ? 32 : 16;
+    static constexpr int TILE = TT * ROW, STAGE = 2 * TILE;
+    static constexpr int STAGES = STAGE <= 4096 ? 6 : 3;
+    static constexpr int WARP_SMEM = STAGES * STAGE;
+    static constexpr int SMEM = KLPM_DECODE_WARPS * WARP_SMEM;
+    static constexpr int CTAS = SMEM <= 100 * 1024 ? 2 : 1;    // per SM
+    static constexpr int HEADS = 8 * NT;
+    static constexpr int PART = HEADS * (2 + DP);
+    static constexpr int QF = QLO ? NT : 1;                    // query operands
 };
 
 __device__ __forceinline__ void token_range(const DecodeArgs& A, int32_t b, int32_t* lo, int32_t* hi) {
@@ -274,82 +320,655 @@ __device__ __forceinline__ void token_range(const DecodeArgs& A, int32_t b, int3
     *hi = n;
     *lo = A.window > 0 && n > A.window ? n - A.window : 0;
 }
-
-// One warp per (sequence, query head), one token after the other: s_t, then the running maximum, sum and output.
-template <int TQ, int TC>
-__global__ void __launch_bounds__(128) decode_kernel(const DecodeArgs A) {
-    using Q = typename Elem<TQ>::T;
-    using C = typename Elem<TC>::T;
-    const int lane = threadIdx.x & 31;
-    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (id >= (int64_t)A.n_seqs * A.q.heads) return;
-    const int32_t b = (int32_t)(id / A.q.heads), h = (int32_t)(id % A.q.heads), g = h / A.group;
-    const Q* q = reinterpret_cast<const Q*>(A.q.p + b * A.q.sr + h * A.q.sh);
-    float x[KV_MAX_HEAD_DIM / 32], o[KV_MAX_HEAD_DIM / 32];
-    for (int j = 0; j < KV_MAX_HEAD_DIM / 32; ++j) {
-        const int d = lane + 32 * j;
-        x[j] = d < A.c.dim ? to_float(q[d]) : 0.0f;
-        o[j] = 0.0f;
-    }
+template <int TT> __device__ __forceinline__ int32_t tiles_of(const DecodeArgs& A, int32_t b, int32_t* first) {
     int32_t lo, hi;
     token_range(A, b, &lo, &hi);
-    float m = -INFINITY, l = 0.0f;
-    for (int32_t t = lo; t < hi; ++t) {
-        const int32_t page = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
-        if ((unsigned)page >= (unsigned)A.c.n_pages) continue;
-        const int32_t at = t & ((1 << A.c.page_shift) - 1);
-        const C* k = reinterpret_cast<const C*>(A.c.k + page * A.c.ks[0] + at * A.c.ks[1] + g * A.c.ks[2]);
-        const C* v = reinterpret_cast<const C*>(A.c.v + page * A.c.vs[0] + at * A.c.vs[1] + g * A.c.vs[2]);
-        float s = 0.0f;
-        for (int j = 0; j < KV_MAX_HEAD_DIM / 32; ++j) if (lane + 32 * j < A.c.dim) s += x[j] * to_float(k[lane + 32 * j]);
-        for (int w = 16; w; w >>= 1) s += __shfl_xor_sync(FULL_MASK, s, w);
-        s *= A.scale * A.c.k_scale;
-        const float m1 = fmaxf(m, s);
-        const float base = m1 == -INFINITY ? 0.0f : m1;
-        const float f = expf(m - base), p = expf(s - base);
-        m = m1;
-        l = l * f + p;
-        for (int j = 0; j < KV_MAX_HEAD_DIM / 32; ++j) if (lane + 32 * j < A.c.dim) o[j] = o[j] * f + p * to_float(v[lane + 32 * j]);
+    *first = lo / TT;
+    return hi > lo ? (hi + TT - 1) / TT - lo / TT : 0;
+}
+__device__ __forceinline__ long long span_of(long long total, int32_t warps) {
+    const long long s = (total + warps - 1) / warps;
+    return s < KLPM_DECODE_MIN_SPAN ? KLPM_DECODE_MIN_SPAN : s;
+}
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {      // bytes 0: 16 zeros, nothing is read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    return v;
+}
+template <bool HALF> __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (HALF)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t e4m3_to_f16(uint32_t two) {           // exact; the low 16 bits hold two values
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));
+    return r;
+}
+// x and y as the sums of two 16-bit numbers each
+template <bool HALF> __device__ __forceinline__ void split2(float x, float y, uint32_t* hi, uint32_t* lo) {
+    if constexpr (HALF) {
+        const __half2 h = __floats2half2_rn(x, y);
+        const float2 f = __half22float2(h);
+        const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+        *hi = *reinterpret_cast<const uint32_t*>(&h); *lo = *reinterpret_cast<const uint32_t*>(&l);
+    } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        const float2 f = __bfloat1622float2(h);
+        const __nv_bfloat162 l = __floats2bfloat162_rn(x - f.x, y - f.y);
+        *hi = *reinterpret_cast<const uint32_t*>(&h); *lo = *reinterpret_cast<const uint32_t*>(&l);
+    }
+}
+// The two halves of an output.  An infinite value times the second half of a probability, which may be 0 or negative, is no number: the
+// first half alone then says what the sum is.
+__device__ __forceinline__ float both(float hi, float lo) {
+    const float x = hi + lo;
+    return x == x ? x : hi;
+}
+__device__ __forceinline__ float exp2_fast(float x) {        // 2 ulp; 2^-inf = 0
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Where chunk c of row r is, in 16-byte units.  Two-byte types: the eight rows of an ldmatrix lie in eight different 16-byte
+// columns.  8-bit keys: lanes read chunks j, j < 4, of rows 2i and 2i+1 together; 8-bit values: chunks n, n+1 (or half chunks) of rows 0, 2, 4, 6.
+template <class X, bool VALUE> __device__ __forceinline__ int place(int r, int c) {
+    if constexpr (!X::E8) return r * X::CH + (c ^ (r & 7));
+    else if constexpr (X::CH == 4) return VALUE ? (r >> 1) * 8 + ((((r & 1) << 2) + c) ^ (((r >> 1) & 3) << 1)) : r * 4 + c;
+    else if constexpr (!VALUE) return r * X::CH + (c ^ ((r & 1) << 2));
+    else if constexpr (X::CH == 8) return r * 8 + (c ^ (((r >> 1) & 3) << 1));
+    else return r * X::CH + (c ^ (((r >> 1) & 1) | (((r >> 2) & 1) << 2)));
+}
+
+// The element of a head that index k (0..15) of step ks of the first product stands for, in groups of two: lane column j holds
+// k = 2j, 2j+1 (part 0) and 2j+8, 2j+9 (part 1).  8-bit keys: 16 consecutive elements per lane serve four steps.
+template <class X> __device__ __forceinline__ int q_element(int ks, int j, int part) {
+    if constexpr (X::E8) return (ks >> 2) * 64 + j * 16 + (ks & 3) * 4 + part * 2;
+    else return ks * 16 + j * 2 + part * 8;
+}
+// The element that column 2j + e of output tile x stands for.
+template <class X> __device__ __forceinline__ int out_element(int x, int j, int e) {
+    if constexpr (X::E8) return (2 * j + e) * (X::DP / 8) + x;
+    else return x * 8 + 2 * j + e;
+}
+
+template <class X> struct Cursor {       // a tile of the batch
+    int32_t b, u, tile, first, end, lo, hi;
+    __device__ __forceinline__ void row(const DecodeArgs& A) {           // to the first tile of sequence b or of the next one that has any
+        for (; b < A.n_seqs; ++b) {
+            token_range(A, b, &lo, &hi);
+            if (hi > lo) break;
+        }
+        first = lo / X::TT;
+        end = (hi + X::TT - 1) / X::TT;
+        tile = first;
+    }
+    __device__ __forceinline__ void next(const DecodeArgs& A) {
+        if (++tile < end) return;
+        tile = first;
+        if (++u < A.units) return;
+        u = 0;
+        ++b;
+        row(A);
+    }
+};
+
+template <class X>
+__global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel(const DecodeArgs A) {
+    using Q = typename Elem<X::TQ>::T;
+    constexpr int TT = X::TT, KS = X::DP / 16, VN = X::DP / 8, TN = TT / 8, NT = X::NT;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ long long s_sum[KLPM_DECODE_WARPS];
+    __shared__ int32_t s_b[KLPM_DECODE_WARPS];
+    __shared__ long long s_rem[KLPM_DECODE_WARPS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    for (int i = tid; i < X::SMEM / 16; i += KLPM_DECODE_WARPS * 32) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);  // elements behind dim stay 0
+    // where each warp starts: every CTA adds up the tiles of all sequences
+    const int32_t per = (A.n_seqs + KLPM_DECODE_WARPS * 32 - 1) / (KLPM_DECODE_WARPS * 32);
+    const int32_t b0 = min((int64_t)tid * per, (int64_t)A.n_seqs), b1 = min((int64_t)b0 + per, (int64_t)A.n_seqs);
+    long long mine = 0;
+    int32_t first;
+    for (int32_t b = b0; b < b1; ++b) mine += tiles_of<TT>(A, b, &first);
+    long long before = mine;
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long v = __shfl_up_sync(FULL_MASK, before, d);
+        if (lane >= d) before += v;
+    }
+    if (lane == 31) s_sum[warp] = before;
+    before -= mine;
+    __syncthreads();
+    long long total = 0;
+    for (int w = 0; w < KLPM_DECODE_WARPS; ++w) {
+        if (w < warp) before += s_sum[w];
+        total += s_sum[w];
+    }
+    if (blockIdx.x == 0) {
+        long long at = before;
+        for (int32_t b = b0; b < b1; ++b) { A.tiles_before[b] = at; at += tiles_of<TT>(A, b, &first); }
+        if (tid == 0) A.tiles_before[A.n_seqs] = total;
+    }
+    total *= A.units;
+    const long long span = span_of(total, A.warps);
+    for (int w = 0; w < KLPM_DECODE_WARPS; ++w) {
+        const long long pos = ((long long)w * gridDim.x + blockIdx.x) * span;
+        if (pos < total && pos >= before * A.units && pos < (before + mine) * A.units) {
+            long long rem = pos - before * A.units;
+            int32_t b = b0;
+            for (;; ++b) {
+                const long long n = (long long)tiles_of<TT>(A, b, &first) * A.units;
+                if (rem < n) break;
+                rem -= n;
+            }
+            s_b[w] = b; s_rem[w] = rem;
+        }
+    }
+    __syncthreads();
+    const int32_t w = warp * gridDim.x + blockIdx.x;          // neighbouring spans on different SMs
+    const long long pos = (long long)w * span;
+    if (pos >= total) return;
+    long long left = min(span, total - pos);                  // tiles to compute
+
+    Cursor<X> ci;                                             // the tile that is loaded next
+    ci.b = s_b[warp]; ci.u = 0;
+    ci.row(A);
+    {
+        const long long rem = s_rem[warp];
+        ci.u = (int32_t)(rem / (ci.end - ci.first));
+        ci.tile = ci.first + (int32_t)(rem % (ci.end - ci.first));
+    }
+    Cursor<X> cc = ci;                                        // the tile that is computed next
+    long long to_load = left;
+
+    const uint32_t ring = smem_addr(smem) + warp * X::WARP_SMEM;
+    const int32_t in_page = (1 << A.c.page_shift) - 1;
+    const int32_t chunks = A.c.dim * (X::E8 ? 1 : 2) / 16;
+    const int my_row = lane / X::CH % TT, my_ch = lane % X::CH;
+    // the page of token `lane` of the tile that is loaded next; -1: nothing there
+    auto page_of = [&]() -> int32_t {
+        const int32_t t = ci.tile * TT + lane;
+        if (lane >= TT || t < ci.lo || t >= ci.hi) return -1;
+        const int32_t p = __ldg(A.table + ci.b * A.table_stride + (t >> A.c.page_shift));
+        return (unsigned)p < (unsigned)A.c.n_pages ? p : -1;
+    };
+    int32_t page = page_of();
+    int slot_in = 0;
+    auto load_tile = [&]() -> unsigned {                      // returns which tokens are there
+        unsigned there = 0;
+        if (to_load > 0) {
+            there = __ballot_sync(FULL_MASK, page >= 0);
+            const uint32_t dk = ring + slot_in * X::STAGE, dv = dk + X::TILE;
+            const int32_t g = ci.u / A.head_tiles;
+            const char* kb = A.c.k + g * A.c.ks[2] + my_ch * 16;
+            const char* vb = A.c.v + g * A.c.vs[2] + my_ch * 16;
+            constexpr int RPI = 32 / X::CH;                   // rows of one instruction
+#pragma unroll
+            for (int i = 0; i < TT / RPI; ++i) {
+                const int r = i * RPI + my_row;
+                const int32_t p = __shfl_sync(FULL_MASK, page, r);
+                const int32_t at = (ci.tile * TT + r) & in_page;
+                const int64_t ok = p < 0 ? 0 : p * A.c.ks[0] + at * A.c.ks[1], ov = p < 0 ? 0 : p * A.c.vs[0] + at * A.c.vs[1];
+                if (my_ch < chunks) {
+                    cp_async16(dk + place<X, false>(r, my_ch) * 16, kb + ok, p < 0 ? 0 : 16);
+                    cp_async16(dv + place<X, true>(r, my_ch) * 16, vb + ov, p < 0 ? 0 : 16);
+                }
+            }
+            if (--to_load > 0) {
+                ci.next(A);
+                page = page_of();
+            }
+            if (++slot_in == X::STAGES) slot_in = 0;
+        }
+        cp_async_commit();
+        return there;
+    };
+
+    const int r8 = lane >> 2, j = lane & 3;
+    const float log2e = 1.4426950408889634f;
+    unsigned there[X::STAGES];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < X::STAGES - 1; ++i) there[i] = load_tile();
+
+    uint32_t qa[X::QF][KS][(NT == 1 && !X::QLO) ? 2 : 4];
+    float coef[NT], m[NT], l[NT], o[NT][VN][4];
+    bool fresh = true, begun_here = false, first_piece = true;
+    int32_t heads = 0;
+    int slot_out = 0;
+    for (; left > 0; --left) {
+        if (fresh) {                                          // a row begins, or the span begins inside one
+            fresh = false;
+            begun_here = cc.tile == cc.first;
+            const int32_t g = cc.u / A.head_tiles, h0 = (cc.u - g * A.head_tiles) * X::HEADS;
+            heads = min(X::HEADS, A.group - h0);
+            const char* qp = A.q.p + cc.b * A.q.sr + (int64_t)(g * A.group + h0) * A.q.sh;
+#pragma unroll
+            for (int f = 0; f < X::QF; ++f) {
+                float up = 1.0f;
+                if constexpr (X::QLO) {
+                    // a power of two brings the largest element next to 2^15: f16 pairs then hold elements down to 2^-39 of it exactly
+                    float most = 0.0f;
+                    if (f * 8 + r8 < heads)
+                        for (int d = j; d < A.c.dim; d += 4) {
+                            const float x = fabsf(to_float(reinterpret_cast<const Q*>(qp + (f * 8 + r8) * A.q.sh)[d]));
+                            if (x < INFINITY) most = fmaxf(most, x);
+                        }
+                    most = fmaxf(most, __shfl_xor_sync(FULL_MASK, most, 1));
+                    most = fmaxf(most, __shfl_xor_sync(FULL_MASK, most, 2));
+                    int e = 0;
+                    if (most > 0.0f) frexpf(most, &e);
+                    e = max(-110, min(110, 15 - e));
+                    up = ldexpf(1.0f, e);
+                    coef[f] = ldexpf(A.scale * A.c.k_scale * log2e, -e);
+                }
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        const int d = q_element<X>(ks, j, part);
+                        auto get = [&](int head, int e) -> float {
+                            return head < heads && d + e < A.c.dim ? to_float(reinterpret_cast<const Q*>(qp + head * A.q.sh)[d + e]) : 0.0f;
+                        };
+                        if constexpr (X::QLO) {
+                            const float x = get(f * 8 + r8, 0) * up, y = get(f * 8 + r8, 1) * up;
+                            split2<true>(x, y, &qa[f][ks][part * 2], &qa[f][ks][part * 2 + 1]);
+                            // (an infinite element minus itself would be NaN: its second half is 0)
+                            const __half2 h = *reinterpret_cast<const __half2*>(&qa[f][ks][part * 2]);
+                            if (__hisinf(h.x)) qa[f][ks][part * 2 + 1] &= 0xffff0000u;
+                            if (__hisinf(h.y)) qa[f][ks][part * 2 + 1] &= 0x0000ffffu;
+                        } else {
+                            uint32_t lo;
+                            split2<X::HALF>(get(r8, 0), get(r8, 1), &qa[0][ks][NT == 1 ? part : part * 2], &lo);
+                            if constexpr (NT == 2) split2<X::HALF>(get(r8 + 8, 0), get(r8 + 8, 1), &qa[0][ks][part * 2 + 1], &lo);
+                        }
+                    }
+            }
+            if constexpr (!X::QLO)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) coef[n] = A.scale * A.c.k_scale * log2e;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                m[n] = -INFINITY; l[n] = 0.0f;
+#pragma unroll
+                for (int x = 0; x < VN; ++x) o[n][x][0] = o[n][x][1] = o[n][x][2] = o[n][x][3] = 0.0f;
+            }
+        }
+        cp_async_wait<X::STAGES - 2>();
+        __syncwarp();                                         // everybody's part of this tile is there, and the tile before it is no longer read
+        there[X::STAGES - 1] = load_tile();
+        const uint32_t sk = ring + slot_out * X::STAGE, sv = sk + X::TILE;
+        if (++slot_out == X::STAGES) slot_out = 0;
+        // s = q . k
+        float s[X::QF][TN][4];
+#pragma unroll
+        for (int f = 0; f < X::QF; ++f)
+#pragma unroll
+            for (int t = 0; t < TN; ++t) s[f][t][0] = s[f][t][1] = s[f][t][2] = s[f][t][3] = 0.0f;
+        auto qk = [&](int t, int ks, uint32_t b0, uint32_t b1) {
+#pragma unroll
+            for (int f = 0; f < X::QF; ++f) {
+                if constexpr (NT == 1 && !X::QLO) mma16816<X::HALF>(s[f][t], qa[f][ks][0], 0u, qa[f][ks][1], 0u, b0, b1);
+                else mma16816<X::HALF>(s[f][t], qa[f][ks][0], qa[f][ks][1], qa[f][ks][2], qa[f][ks][3], b0, b1);
+            }
+        };
+        if constexpr (X::E8) {
+#pragma unroll
+            for (int hb = 0; hb < X::DP / 64; ++hb) {
+                if (hb * 64 >= A.c.dim) break;
+#pragma unroll
+                for (int t = 0; t < TN; ++t) {
+                    const uint4 v = lds128(sk + place<X, false>(t * 8 + r8, hb * 4 + j) * 16);
+                    qk(t, hb * 4 + 0, e4m3_to_f16(v.x), e4m3_to_f16(v.x >> 16));
+                    qk(t, hb * 4 + 1, e4m3_to_f16(v.y), e4m3_to_f16(v.y >> 16));
+                    qk(t, hb * 4 + 2, e4m3_to_f16(v.z), e4m3_to_f16(v.z >> 16));
+                    qk(t, hb * 4 + 3, e4m3_to_f16(v.w), e4m3_to_f16(v.w >> 16));
+                }
+            }
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if (ks * 16 >= A.c.dim) break;
+#pragma unroll
+                for (int t = 0; t < TN; t += 2) {
+                    uint32_t b[4];          // tokens 0-7 and 8-15 of the pair, elements 0-7 and 8-15 of the step
+                    ldmatrix4(b, sk + place<X, false>(t * 8 + (lane & 7) + ((lane >> 4) << 3), ks * 2 + ((lane >> 3) & 1)) * 16);
+                    qk(t, ks, b[0], b[1]);
+                    qk(t + 1, ks, b[2], b[3]);
+                }
+            }
+        }
+        // p = 2^(s - m), in place
+        const unsigned have = there[0];
+        uint32_t pa[NT][TN / 2][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float z[TN][2];
+            float top = m[n];
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = X::QLO ? s[n * (X::QF - 1)][t][e] + s[n * (X::QF - 1)][t][e + 2] : s[0][t][n * 2 + e];
+                    x = (have >> (t * 8 + 2 * j + e)) & 1 ? x * coef[n] : -INFINITY;
+                    z[t][e] = x;
+                    top = fmaxf(top, x);
+                }
+            if (A.weight && n * 8 + r8 < heads) {
+                const int32_t g = cc.u / A.head_tiles, h = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS + n * 8 + r8;
+                float* row = A.score + ((int64_t)cc.b * A.q.heads + h) * A.score_len + (int64_t)cc.tile * TT + 2 * j;
+#pragma unroll
+                for (int t = 0; t < TN; ++t) *reinterpret_cast<float2*>(row + t * 8) = make_float2(z[t][0], z[t][1]);
+            }
+            top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 2));
+            if (__any_sync(FULL_MASK, top > m[n])) {          // rare after the first tiles
+                const float f = m[n] == -INFINITY ? 0.0f : exp2_fast(m[n] - top);
+                l[n] *= f;
+#pragma unroll
+                for (int x = 0; x < VN; ++x) { o[n][x][0] *= f; o[n][x][1] *= f; o[n][x][2] *= f; o[n][x][3] *= f; }
+                m[n] = top;
+            }
+            const float base = m[n] == -INFINITY ? 0.0f : m[n] - (X::HALF ? 15.0f : 0.0f);
+#pragma unroll
+            for (int t = 0; t < TN; ++t) {
+                const float p0 = exp2_fast(z[t][0] - base), p1 = exp2_fast(z[t][1] - base);
+                l[n] += p0 + p1;
+                split2<X::HALF>(p0, p1, &pa[n][t / 2][(t & 1) * 2], &pa[n][t / 2][(t & 1) * 2 + 1]);
+            }
+        }
+        // o += p . v
+        if constexpr (X::E8) {
+#pragma unroll
+            for (int kt = 0; kt < TN / 2; ++kt) {
+                const int r0 = kt * 16 + 2 * j;
+                constexpr int W = X::DP / 32;                 // words of a lane's elements
+                uint32_t v[4][W];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = r0 + (i & 1) + (i >> 1) * 8;
+                    if constexpr (X::CH == 4) {
+                        const uint2 a = lds64(sv + place<X, true>(r, r8 >> 1) * 16 + (r8 & 1) * 8);
+                        v[i][0] = a.x; v[i][1] = a.y;
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < W / 4; ++c) {
+                            const uint4 a = lds128(sv + place<X, true>(r, r8 * (W / 4) + c) * 16);
+                            v[i][c * 4] = a.x; v[i][c * 4 + 1] = a.y; v[i][c * 4 + 2] = a.z; v[i][c * 4 + 3] = a.w;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < VN; x += 2) {
+                    // bytes x, x+1 of two tokens each: (token 0, token 1) of element x, then of x+1
+                    const uint32_t sel = x & 2 ? 0x7362 : 0x5140;
+                    const uint32_t a = __byte_perm(v[0][x / 4], v[1][x / 4], sel), b = __byte_perm(v[2][x / 4], v[3][x / 4], sel);
+                    const uint32_t a0 = e4m3_to_f16(a), a1 = e4m3_to_f16(a >> 16), b0 = e4m3_to_f16(b), b1 = e4m3_to_f16(b >> 16);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        mma16816<true>(o[n][x], pa[n][kt][0], pa[n][kt][1], pa[n][kt][2], pa[n][kt][3], a0, b0);
+                        mma16816<true>(o[n][x + 1], pa[n][kt][0], pa[n][kt][1], pa[n][kt][2], pa[n][kt][3], a1, b1);
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int kt = 0; kt < TN / 2; ++kt)
+#pragma unroll
+                for (int x = 0; x < VN; x += 2) {
+                    if (x * 8 >= A.c.dim) break;
+                    uint32_t b[4];          // tokens 0-7 and 8-15, elements 0-7 of the tile x and of x+1
+                    ldmatrix4_trans(b, sv + place<X, true>(kt * 16 + (lane & 15), x + (lane >> 4)) * 16);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        mma16816<X::HALF>(o[n][x], pa[n][kt][0], pa[n][kt][1], pa[n][kt][2], pa[n][kt][3], b[0], b[1]);
+                        mma16816<X::HALF>(o[n][x + 1], pa[n][kt][0], pa[n][kt][1], pa[n][kt][2], pa[n][kt][3], b[2], b[3]);
+                    }
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < X::STAGES - 1; ++i) there[i] = there[i + 1];
+        // the row ends, or the span
+        const bool row_ends = cc.tile + 1 == cc.end;
+        if (row_ends || left == 1) {
+            const int32_t g = cc.u / A.head_tiles, h0 = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS;
+            const bool whole = begun_here && row_ends;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float sum = l[n];
+                sum += __shfl_xor_sync(FULL_MASK, sum, 1);
+                sum += __shfl_xor_sync(FULL_MASK, sum, 2);
+                const int hd = n * 8 + r8;
+                if (hd >= heads) continue;
+                const float off = X::HALF ? 15.0f : 0.0f;
+                if (whole) {
+                    const int64_t row = (int64_t)cc.b * A.q.heads + h0 + hd;
+                    Q* out = reinterpret_cast<Q*>(A.out.p + cc.b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
+                    const float f = sum == 0.0f ? 0.0f : A.c.v_scale / sum;
+#pragma unroll
+                    for (int x = 0; x < VN; ++x)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int d = out_element<X>(x, j, e);
+                            if (d < A.c.dim) out[d] = from_float<Q>(sum == 0.0f ? 0.0f : both(o[n][x][e], o[n][x][e + 2]) * f);
+                        }
+                    if (j == 0) {
+                        const float y = sum == 0.0f ? -INFINITY : m[n] - off + log2f(sum);
+                        if (A.lse) A.lse[row] = y * 0.6931471805599453f;
+                        if (A.weight) A.lse2[row] = y;
+                    }
+                } else {
+                    float* part = A.part + ((int64_t)w * 2 + (first_piece ? 0 : 1)) * X::PART;
+                    if (j == 0) { part[hd] = m[n] - off; part[X::HEADS + hd] = sum; }
+                    part += 2 * X::HEADS + hd * X::DP;
+#pragma unroll
+                    for (int x = 0; x < VN; ++x)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int d = out_element<X>(x, j, e);
+                            if (d < A.c.dim) part[d] = both(o[n][x][e], o[n][x][e + 2]);
+                        }
+                }
+            }
+            fresh = true;
+            first_piece = false;
+        }
+        if (left > 1) cc.next(A);
+    }
+}
+
+// Rows that were cut into parts, and rows with nothing to attend to.  One row (sequence, query head) per `WPR` warps: few rows have
+// many parts each (WPR = 8: the warps share them), many rows few.
+template <class X, int WPR>
+__global__ void __launch_bounds__(256) decode_join_kernel(const DecodeArgs A) {
+    using Q = typename Elem<X::TQ>::T;
+    constexpr int PER = X::DP / 32;
+    __shared__ float s_m[8], s_l[8], s_o[WPR == 1 ? 1 : 8][X::DP];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t row = WPR == 8 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + warp;
+    if (row >= (int64_t)A.n_seqs * A.q.heads) return;
+    const int32_t b = (int32_t)(row / A.q.heads), h = (int32_t)(row % A.q.heads), g = h / A.group, i = h - g * A.group;
+    const int32_t u = g * A.head_tiles + i / X::HEADS, hd = i % X::HEADS;
+    const long long t0 = A.tiles_before[b], tiles = A.tiles_before[b + 1] - t0;
+    const long long span = span_of(A.tiles_before[A.n_seqs] * A.units, A.warps);
+    const long long R = t0 * A.units + u * tiles, E = R + tiles;
+    const long long w0 = R / span, w1 = (E - 1) / span;
+    if (tiles > 0 && w0 == w1) return;                       // decode_kernel has written it
+    const int part_of = WPR == 8 ? warp : 0;
+    float m = -INFINITY, l = 0.0f, o[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) o[k] = 0.0f;
+    if (tiles > 0) {
+        const long long first = w0 * span == R ? w0 * 2 : w0 * 2 + 1;
+        for (long long w = w0 + part_of; w <= w1; w += WPR) {
+            const float* p = A.part + (w == w0 ? first : w * 2) * X::PART;
+            const float pm = p[hd], pl = p[X::HEADS + hd];
+            float v[PER];
+#pragma unroll
+            for (int k = 0; k < PER; ++k) v[k] = lane + 32 * k < A.c.dim ? p[2 * X::HEADS + hd * X::DP + lane + 32 * k] : 0.0f;
+            const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.0f : top;
+            const float f = exp2_fast(m - base), pf = exp2_fast(pm - base);
+            m = top;
+            l = l * f + pl * pf;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) o[k] = o[k] * f + v[k] * pf;
+        }
+    }
+    if constexpr (WPR == 8) {
+        if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
+#pragma unroll
+        for (int k = 0; k < PER; ++k) s_o[warp][lane + 32 * k] = o[k];
+        __syncthreads();
+        if (warp) return;
+        float top = -INFINITY;
+        for (int w = 0; w < 8; ++w) top = fmaxf(top, s_m[w]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        l = 0.0f;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) o[k] = 0.0f;
+        for (int w = 0; w < 8; ++w) {
+            const float f = exp2_fast(s_m[w] - base);
+            l += s_l[w] * f;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) o[k] += s_o[w][lane + 32 * k] * f;
+        }
+        m = top;
     }
     Q* out = reinterpret_cast<Q*>(A.out.p + b * A.out.sr + h * A.out.sh);
-    const float r = l == 0.0f ? 0.0f : A.c.v_scale / l;
-    for (int j = 0; j < KV_MAX_HEAD_DIM / 32; ++j) if (lane + 32 * j < A.c.dim) out[lane + 32 * j] = from_float<Q>(l == 0.0f ? 0.0f : o[j] * r);
-    if (lane == 0) A.lse[id] = l == 0.0f ? -INFINITY : m + logf(l);
+    const float f = l == 0.0f ? 0.0f : A.c.v_scale / l;
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+        if (lane + 32 * k < A.c.dim) out[lane + 32 * k] = from_float<Q>(l == 0.0f ? 0.0f : o[k] * f);
+    if (lane == 0) {
+        const float y = l == 0.0f ? -INFINITY : m + log2f(l);
+        if (A.lse) A.lse[row] = y * 0.6931471805599453f;
+        if (A.weight) A.lse2[row] = y;
+    }
 }
 
-// One warp per (sequence, cache head, token): the scores once more, now that the sums are known.
-template <int TQ, int TC>
-__global__ void __launch_bounds__(128) decode_weight_kernel(const DecodeArgs A) {
-    using Q = typename Elem<TQ>::T;
-    using C = typename Elem<TC>::T;
+// What every token received, from the scores that decode_kernel kept: a warp takes a span of tiles of the batch, in the order (sequence,
+// cache head, tile).  One thread adds up a token's heads, so that the order of the sum is fixed.
+template <int TT>
+__global__ void __launch_bounds__(256) decode_weight_kernel(const DecodeArgs A) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31;
-    const int32_t t = blockIdx.x * 4 + (threadIdx.x >> 5), g = blockIdx.y, b = blockIdx.z;
-    int32_t lo, hi;
-    token_range(A, b, &lo, &hi);
-    if (t < lo || t >= hi) return;
-    const int32_t page = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
-    if ((unsigned)page >= (unsigned)A.c.n_pages) return;
-    const int32_t at = t & ((1 << A.c.page_shift) - 1);
-    const C* k = reinterpret_cast<const C*>(A.c.k + page * A.c.ks[0] + at * A.c.ks[1] + g * A.c.ks[2]);
-    float sum = 0.0f;
-    for (int32_t h = g * A.group; h < (g + 1) * A.group; ++h) {
-        const Q* q = reinterpret_cast<const Q*>(A.q.p + b * A.q.sr + h * A.q.sh);
-        float s = 0.0f;
-        for (int d = lane; d < A.c.dim; d += 32) s += to_float(q[d]) * to_float(k[d]);
-        for (int w = 16; w; w >>= 1) s += __shfl_xor_sync(FULL_MASK, s, w);
-        const float lse = A.lse[(int64_t)b * A.q.heads + h];
-        if (lse != -INFINITY) sum += expf(s * A.scale * A.c.k_scale - lse);
+    const int32_t w = blockIdx.x * 8 + (threadIdx.x >> 5), warps = gridDim.x * 8;
+    const long long total = A.tiles_before[A.n_seqs] * A.c.n_heads, span = span_of(total, warps);
+    long long pos = w * span;
+    const long long stop = min(pos + span, total);
+    if (pos >= stop) return;
+    int32_t b = 0, last = A.n_seqs;                          // the sequence: tiles_before[b] * heads <= pos < tiles_before[b + 1] * heads
+    while (last - b > 1) {
+        const int32_t mid = b + (last - b) / 2;
+        if (A.tiles_before[mid] * A.c.n_heads <= pos) b = mid;
+        else last = mid;
     }
-    if (lane == 0) A.weight[b * A.ws[0] + g * A.ws[1] + t] += sum;
+    while (pos < stop) {
+        const long long t0 = A.tiles_before[b], tiles = A.tiles_before[b + 1] - t0;
+        if (tiles == 0) { ++b; continue; }
+        const long long in = pos - t0 * A.c.n_heads;
+        if (in >= tiles * A.c.n_heads) { ++b; continue; }
+        const int32_t g = (int32_t)(in / tiles);
+        const long long at = in - g * tiles, n = min(tiles - at, stop - pos);
+        int32_t lo, hi;
+        token_range(A, b, &lo, &hi);
+        const int32_t first = lo / TT, from = (int32_t)max((long long)lo, (first + at) * TT), to = (int32_t)min((long long)hi, (first + at + n) * TT);
+        const float* score = A.score + ((int64_t)b * A.q.heads + g * A.group) * A.score_len;
+        const float* norm = A.lse2 + (int64_t)b * A.q.heads + g * A.group;
+        float* weight = A.weight + b * A.ws[0] + g * A.ws[1];
+        for (int32_t t = from + lane; t < to; t += 32) {
+            float sum = 0.0f;
+            for (int32_t i = 0; i < A.group; ++i) {
+                const float s = score[i * A.score_len + t], z = norm[i];
+                if (s != -INFINITY) sum += exp2_fast(s - z);      // (z is -inf only where every s is)
+            }
+            if (sum != 0.0f) weight[t] += sum;
+        }
+        pos += n;
+    }
 }
 
-template <int TQ, int TC> void launch_decode(const DecodeArgs& A, cudaStream_t s) {
-    const int64_t warps = (int64_t)A.n_seqs * A.q.heads;
-    decode_kernel<TQ, TC><<<(unsigned)((warps + 3) / 4), 128, 0, s>>>(A);
-    if (A.weight) {
-        const dim3 grid((A.max_tokens + 3) / 4, A.c.n_heads, A.n_seqs);
-        decode_weight_kernel<TQ, TC><<<grid, 128, 0, s>>>(A);
-    }
+inline int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
+
+// The workspace of a call: what decode_kernel leaves for the kernels after it.
+struct DecodeSpace { int64_t lse2, part, score, score_len, bytes; };
+DecodeSpace decode_space(int64_t n_seqs, int64_t heads, int64_t max_tokens, int64_t warps, int64_t part, bool weight) {
+    DecodeSpace s;
+    s.lse2 = up256((n_seqs + 1) * 8);
+    s.part = s.lse2 + (weight ? up256(n_seqs * heads * 4) : 0);
+    s.score = s.part + up256(warps * 2 * part * 4);
+    s.score_len = (max_tokens + 31) / 32 * 32;
+    s.bytes = s.score + (weight ? up256(n_seqs * heads * s.score_len * 4) : 0);
+    return s;
+}
+
+template <typename... P> rt_status launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, cudaStream_t s, P... args) {
+    // its CTAs may be set up while the kernel before it in the stream still runs; griddepcontrol.wait in it waits for that one's end
+    cudaLaunchConfig_t c = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    c.gridDim = grid; c.blockDim = dim3(threads); c.stream = s; c.attrs = at; c.numAttrs = 1;
+    CK(cudaLaunchKernelEx(&c, kernel, args...));
+    return RT_OK;
+}
+
+template <class X> rt_status launch_decode(DecodeArgs& A, char* work, cudaStream_t s) {
+    A.warps = KLPM_SMS * X::CTAS * KLPM_DECODE_WARPS;
+    A.head_tiles = (A.group + X::HEADS - 1) / X::HEADS;
+    A.units = A.c.n_heads * A.head_tiles;
+    const DecodeSpace W = decode_space(A.n_seqs, A.q.heads, A.max_tokens, A.warps, X::PART, A.weight != nullptr);
+    A.tiles_before = (long long*)work; A.lse2 = (float*)(work + W.lse2); A.part = (float*)(work + W.part); A.score = (float*)(work + W.score);
+    A.score_len = W.score_len;
+    CK(cudaFuncSetAttribute(decode_kernel<X>, cudaFuncAttributeMaxDynamicSharedMemorySize, X::SMEM));
+    decode_kernel<X><<<KLPM_SMS * X::CTAS, KLPM_DECODE_WARPS * 32, X::SMEM, s>>>(A);
+    CK(cudaGetLastError());
+    const int64_t rows = (int64_t)A.n_seqs * A.q.heads;
+    // a row has 1184 / rows parts or so: with fewer rows than that, eight warps share a row's
+    rt_status st = rows <= A.warps ? launch_after(decode_join_kernel<X, 8>, dim3((unsigned)rows), 256, s, A)
+                                   : launch_after(decode_join_kernel<X, 1>, dim3((unsigned)((rows + 7) / 8)), 256, s, A);
+    if (st || !A.weight) return st;
+    return launch_after(decode_weight_kernel<X::TT>, dim3(KLPM_SMS * 4), 256, s, A);
+}
+
+// The instance for a call: DP = dim rounded up to 64, 128 or 256, 8 or 16 query heads per unit.  (16 where the registers hold them: not for wide
+// heads, and not where the query is kept as two numbers.)
+template <int TQ, int TC, int DP, class F> auto for_heads(int32_t group, F f) {
+    if constexpr (DP <= 64 || (DP == 128 && !(TQ == KV_BF16 && TC == KV_E4M3)))
+        if (group > 8) return f(Dec<TQ, TC, DP, 2>());
+    return f(Dec<TQ, TC, DP, 1>());
+}
+template <int TQ, int TC, class F> auto for_dim(int32_t dim, int32_t group, F f) {
+    if (dim <= 64) return for_heads<TQ, TC, 64>(group, f);
+    if (dim <= 128) return for_heads<TQ, TC, 128>(group, f);
+    return for_heads<TQ, TC, 256>(group, f);
+}
+template <class F> auto for_decode(int tq, int tc, int32_t dim, int32_t group, F f) {
+    if (tq == KV_BF16) return tc == KV_E4M3 ? for_dim<KV_BF16, KV_E4M3>(dim, group, f) : for_dim<KV_BF16, KV_BF16>(dim, group, f);
+    return tc == KV_E4M3 ? for_dim<KV_F16, KV_E4M3>(dim, group, f) : for_dim<KV_F16, KV_F16>(dim, group, f);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -543,11 +1162,21 @@ rt_status kv_rope_append(const kv_cache* cache, const kv_rope* rope, const int32
 }
 
 int64_t kv_decode_workspace(const kv_cache* cache, int32_t n_seqs, int32_t n_q_heads, int32_t max_pages, int32_t with_weight) {
-    (void)with_weight;
     const rt_status st = check_cache(cache);
     if (st) return st;
     if (n_seqs < 0 || n_q_heads < 1 || max_pages < 0 || n_q_heads % cache->n_heads) return RT_ERR_INVALID;
-    return ((int64_t)n_seqs * n_q_heads * 4 + 255) / 256 * 256;
+    if (n_seqs > 65535 || n_q_heads > 65535 || (int64_t)max_pages * cache->page_size > KLPM_MAX_TOKENS) return RT_ERR_TOO_LARGE;
+    // (the query's type is not known here: the larger of what either needs next to an 8-bit cache)
+    int64_t bytes = 0;
+    for (int tq = KV_BF16; tq <= KV_F16; ++tq) {
+        if (cache->dtype != KV_E4M3 && cache->dtype != tq) continue;
+        const int64_t n = for_decode(tq, cache->dtype, cache->head_dim, n_q_heads / cache->n_heads, [&](auto x) {
+            using X = decltype(x);
+            return decode_space(n_seqs, n_q_heads, (int64_t)max_pages * cache->page_size, KLPM_SMS * X::CTAS * KLPM_DECODE_WARPS, X::PART, with_weight != 0).bytes;
+        });
+        bytes = n > bytes ? n : bytes;
+    }
+    return bytes;
 }
 
 rt_status kv_decode(const kv_cache* cache, const kv_rows* q, const kv_rows* out, int32_t n_seqs, const int32_t* d_page_table,
@@ -572,18 +1201,12 @@ rt_status kv_decode(const kv_cache* cache, const kv_rows* q, const kv_rows* out,
     A.c = cache_dev(cache); A.q = rows_dev(q); A.out = rows_dev(out);
     A.table = d_page_table; A.len = d_lengths; A.table_stride = table_stride; A.n_seqs = n_seqs;
     A.group = q->n_heads / cache->n_heads; A.max_tokens = max_pages * cache->page_size; A.window = window; A.scale = scale;
-    A.lse = d_lse ? d_lse : (float*)d_workspace;
+    A.lse = d_lse;
     A.weight = A.max_tokens > 0 ? d_weight : nullptr;
     A.ws[0] = d_weight ? weight_stride[0] : 0; A.ws[1] = d_weight ? weight_stride[1] : 0;
-    cudaStream_t s = (cudaStream_t)stream;
-    switch (q->dtype * 4 + cache->dtype) {
-        case KV_BF16 * 4 + KV_BF16: launch_decode<KV_BF16, KV_BF16>(A, s); break;
-        case KV_BF16 * 4 + KV_E4M3: launch_decode<KV_BF16, KV_E4M3>(A, s); break;
-        case KV_F16 * 4 + KV_F16: launch_decode<KV_F16, KV_F16>(A, s); break;
-        default: launch_decode<KV_F16, KV_E4M3>(A, s); break;
-    }
-    CK(cudaGetLastError());
-    return RT_OK;
+    return for_decode(q->dtype, cache->dtype, cache->head_dim, A.group, [&](auto x) {
+        return launch_decode<decltype(x)>(A, (char*)d_workspace, (cudaStream_t)stream);
+    });
 }
 
 rt_status kv_evict(const kv_cache* cache, const float* d_weight, const int64_t* weight_stride, int32_t n_seqs,
