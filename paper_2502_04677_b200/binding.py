@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -418,26 +419,29 @@ class kv_rope(ctypes.Structure):
     _fields_ = [("d_turns", _vp), ("rot_dim", _i32), ("interleaved", _i32), ("factor", ctypes.c_float)]
 
 
-_pc, _pr, _p2 = ctypes.POINTER(kv_cache), ctypes.POINTER(kv_rows), ctypes.POINTER(_i64)
 _f32, _f64 = ctypes.c_float, ctypes.c_double
+# structs are passed as addresses or as packed bytes: building a ctypes object per argument costs more than a small call's launches
 _lib.kv_rope_table.restype = _i32
 _lib.kv_rope_table.argtypes = [_vp, _i32, _f64, _i32, _f64, _f64, _f64, _f64, ctypes.POINTER(_f32), _vp]
 _lib.kv_rope_append.restype = _i32
-_lib.kv_rope_append.argtypes = [_pc, ctypes.POINTER(kv_rope), _vp, _vp, _i32, _pr, _pr, _pr, _pr, _vp]
+_lib.kv_rope_append.argtypes = [_vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp]
 _lib.kv_decode_workspace.restype = _i64
-_lib.kv_decode_workspace.argtypes = [_pc, _i32, _i32, _i32, _i32]
+_lib.kv_decode_workspace.argtypes = [_vp, _i32, _i32, _i32, _i32]
 _lib.kv_decode.restype = _i32
-_lib.kv_decode.argtypes = [_pc, _pr, _pr, _i32, _vp, _i64, _i32, _vp, _f32, _i32, _vp, _vp, _p2, _vp, _i64, _vp]
+_lib.kv_decode.argtypes = [_vp, _vp, _vp, _i32, _vp, _i64, _i32, _vp, _f32, _i32, _vp, _vp, _vp, _vp, _i64, _vp]
 _lib.kv_evict.restype = _i32
-_lib.kv_evict.argtypes = [_pc, _vp, _p2, _i32, _vp, _i64, _i32, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _p2, _i32, _vp, _vp]
+_lib.kv_evict.argtypes = [_vp, _vp, _vp, _i32, _vp, _i64, _i32, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _vp]
+_pack_rows, _pack_strides = struct.Struct("Pii2q").pack, struct.Struct("2q").pack      # kv_rows; int64[2]
 
 KV_EXPORTS = ["kv_rope_table", "kv_rope_append", "kv_decode_workspace", "kv_decode", "kv_evict"]
 
 
-def _here(device: torch.device) -> None:
-    """The calls launch on the current device's current stream: tensors of another device are refused."""
-    if device.index != torch.cuda.current_device():
-        raise ValueError("tensors are on %s, the current device is cuda:%d" % (device, torch.cuda.current_device()))
+def _stream_of(device: torch.device) -> int:
+    """The current stream's handle.  The calls launch on the current device: tensors of another one are refused."""
+    here = torch.cuda.current_device()
+    if device.index != here:
+        raise ValueError("tensors are on %s, the current device is cuda:%d" % (device, here))
+    return torch._C._cuda_getCurrentRawStream(here)
 
 
 class KvCache:
@@ -460,6 +464,7 @@ class KvCache:
             raise ValueError("a dimension of the cache is too large")
         self.c = kv_cache(k.data_ptr(), v.data_ptr(), _KV_TYPES[k.dtype], *k.shape, float(k_scale), float(v_scale),
                           (_i64 * 3)(*k.stride()[:3]), (_i64 * 3)(*v.stride()[:3]))
+        self.p = ctypes.addressof(self.c)
 
 
 class Rope:
@@ -468,6 +473,7 @@ class Rope:
     def __init__(self, turns: torch.Tensor, rot_dim: int, interleaved: bool, factor: float):
         self.turns, self.factor = turns, factor
         self.c = kv_rope(turns.data_ptr(), rot_dim, int(interleaved), factor)
+        self.p = ctypes.addressof(self.c)
 
 
 def kv_rope_table(rot_dim: int, theta: float = 10_000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
@@ -477,25 +483,37 @@ def kv_rope_table(rot_dim: int, theta: float = 10_000.0, interleaved: bool = Fal
     if scaling not in ROPE_SCALINGS:
         raise ValueError("scaling must be one of %s" % ", ".join(sorted(ROPE_SCALINGS)))
     turns = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.float64, device=device)
-    _here(turns.device)
+    stream = _stream_of(turns.device)
     f = _f32()
     _check(_lib.kv_rope_table(turns.data_ptr(), int(rot_dim), float(theta), ROPE_SCALINGS[scaling], float(factor), float(original_len),
-                              float(beta_fast), float(beta_slow), ctypes.byref(f), _stream()), "kv_rope_table")
+                              float(beta_fast), float(beta_slow), ctypes.byref(f), stream), "kv_rope_table")
     return Rope(turns, int(rot_dim), interleaved, f.value)
 
 
-def _rows(t: torch.Tensor, cache: KvCache, n: int, name: str) -> kv_rows:
-    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != cache.head_dim or (t.stride(2) != 1 and t.shape[2] > 1):
+def _rows(t: torch.Tensor, cache: KvCache, n: int, name: str) -> bytes:
+    shape, stride, dtype = t.shape, t.stride(), _KV_TYPES.get(t.dtype)
+    if len(shape) != 3 or shape[0] != n or shape[2] != cache.head_dim or (stride[2] != 1 and shape[2] > 1):
         raise ValueError("%s must be [%d, heads, %d] with contiguous head_dim" % (name, n, cache.head_dim))
-    if t.device != cache.device or t.dtype not in _KV_TYPES:
+    if dtype is None or t.device != cache.device:
         raise ValueError("%s must be a floating-point tensor on the cache's device" % name)
-    return kv_rows(t.data_ptr(), _KV_TYPES[t.dtype], t.shape[1], (_i64 * 2)(t.stride(0), t.stride(1)))
+    return _pack_rows(t.data_ptr(), dtype, shape[1], stride[0], stride[1])
 
 
-def _on(t: torch.Tensor, device: torch.device, name: str) -> torch.Tensor:
-    if t.device != device:
+def _ints(t: torch.Tensor, cache: KvCache, n: int, name: str) -> int:
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of %d elements" % (name, n))
+    if t.device != cache.device:
         raise ValueError("%s must be on the cache's device" % name)
-    return t
+    return t.data_ptr()
+
+
+def _pages(t: torch.Tensor, cache: KvCache, n: int, name: str):
+    """Pointer, row stride and width of a page table."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != n or t.device != cache.device:
+        raise ValueError("%s must have one row per sequence, on the cache's device" % name)
+    p, stride = _table(t, name)
+    return p, stride, shape[1]
 
 
 def kv_rope_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None,
@@ -503,36 +521,41 @@ def kv_rope_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torc
     """Rotate q [n, q_heads, head_dim] into q_out and k by positions (int32[n]), and store k and v [n, n_heads, head_dim] at slots
     (int32[n]) of the cache.  q_out may be q.  Without rope nothing is rotated; rows with a slot out of range are not stored."""
     n = slots.numel()
-    _here(cache.device)
-    _on(slots, cache.device, "slots")
-    if rope is not None and (positions is None or positions.numel() != n):
-        raise ValueError("rope needs one position per row")
-    if positions is not None:
-        _on(positions, cache.device, "positions")
+    at = p = None
     if rope is not None:
-        _on(rope.turns, cache.device, "the table of rope")
-    if (q is None) != (q_out is None):
+        if positions is None:
+            raise ValueError("rope needs one position per row")
+        if rope.turns.device != cache.device:
+            raise ValueError("the table of rope must be on the cache's device")
+        p = rope.p
+    if positions is not None:
+        at = _ints(positions, cache, n, "positions")
+    rq = ro = None
+    if q is not None and q_out is not None:
+        rq = _rows(q, cache, n, "q")
+        ro = rq if q_out is q else _rows(q_out, cache, n, "q_out")
+    elif q is not None or q_out is not None:
         raise ValueError("q and q_out go together")
-    _check(_lib.kv_rope_append(cache.c, rope.c if rope is not None else None, _dev(positions, torch.int32, "positions", True),
-                               _dev(slots, torch.int32, "slots"), n, _rows(q, cache, n, "q") if q is not None else None,
-                               _rows(q_out, cache, n, "q_out") if q is not None else None, _rows(k, cache, n, "k"),
-                               _rows(v, cache, n, "v"), _stream()), "kv_rope_append")
+    _check(_lib.kv_rope_append(cache.p, p, at, _ints(slots, cache, n, "slots"), n, rq, ro, _rows(k, cache, n, "k"), _rows(v, cache, n, "v"),
+                               _stream_of(cache.device)), "kv_rope_append")
 
 
 def kv_decode_workspace(cache: KvCache, n_seqs: int, n_q_heads: int, max_pages: int, with_weight: bool = False) -> torch.Tensor:
     """Device memory for the workspace of a kv_decode of these sizes.  One call uses it at a time."""
-    n = _lib.kv_decode_workspace(cache.c, int(n_seqs), int(n_q_heads), int(max_pages), int(with_weight))
+    n = _lib.kv_decode_workspace(cache.p, int(n_seqs), int(n_q_heads), int(max_pages), int(with_weight))
     if n < 0:
         _check(n, "kv_decode_workspace")
     return torch.empty(max(n, 256), dtype=torch.uint8, device=cache.device)
 
 
 def _weight(t: torch.Tensor, cache: KvCache, n: int, least: int, name: str):
-    if t.dtype is not torch.float32 or t.dim() != 3 or t.shape[0] != n or t.shape[1] != cache.n_heads or t.shape[2] < least \
-            or (t.stride(2) != 1 and t.shape[2] > 1):
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not torch.float32 or len(shape) != 3 or shape[0] != n or shape[1] != cache.n_heads or shape[2] < least \
+            or (stride[2] != 1 and shape[2] > 1):
         raise ValueError("%s must be a float32 [%d, %d, >= %d] tensor with contiguous rows" % (name, n, cache.n_heads, least))
-    _on(t, cache.device, name)
-    return t.data_ptr(), (_i64 * 2)(t.stride(0), t.stride(1))
+    if t.device != cache.device:
+        raise ValueError("%s must be on the cache's device" % name)
+    return t.data_ptr(), _pack_strides(stride[0], stride[1])
 
 
 def kv_decode(cache: KvCache, q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, out: torch.Tensor,
@@ -543,22 +566,18 @@ def kv_decode(cache: KvCache, q: torch.Tensor, page_table: torch.Tensor, lengths
     weight float32[n_seqs, n_heads, max_pages * page_size] is increased by what every cached token received.  Without a
     workspace (kv_decode_workspace) the call takes one from torch's allocator."""
     n = lengths.numel()
-    _here(cache.device)
-    if page_table.dim() != 2 or page_table.shape[0] != n:
-        raise ValueError("page_table must have one row per sequence")
-    for t, name in ((page_table, "page_table"), (lengths, "lengths")):
-        _on(t, cache.device, name)
-    table, stride = _table(page_table, "page_table")
-    max_pages = page_table.shape[1]
-    if lse is not None and _on(lse, cache.device, "lse").shape != q.shape[:2]:
-        raise ValueError("lse must be [n_seqs, q_heads]")
+    table, stride, max_pages = _pages(page_table, cache, n, "page_table")
+    rq = _rows(q, cache, n, "q")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.device != cache.device):
+        raise ValueError("lse must be a contiguous float32 [n_seqs, q_heads] tensor on the cache's device")
     w, ws = _weight(weight, cache, n, max_pages * cache.page_size, "weight") if weight is not None else (None, None)
     if workspace is None:
         workspace = kv_decode_workspace(cache, n, q.shape[1], max_pages, weight is not None)
-    _check(_lib.kv_decode(cache.c, _rows(q, cache, n, "q"), _rows(out, cache, n, "out"), n, table, stride, max_pages,
-                          _dev(lengths, torch.int32, "lengths"), cache.head_dim ** -0.5 if scale is None else float(scale), int(window),
-                          _dev(lse, torch.float32, "lse", True), w, ws,
-                          _dev(_on(workspace, cache.device, "workspace"), torch.uint8, "workspace"), workspace.numel(), _stream()), "kv_decode")
+    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.device != cache.device:
+        raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
+    _check(_lib.kv_decode(cache.p, rq, _rows(out, cache, n, "out"), n, table, stride, max_pages, _ints(lengths, cache, n, "lengths"),
+                          cache.head_dim ** -0.5 if scale is None else scale, window, lse.data_ptr() if lse is not None else None, w, ws,
+                          workspace.data_ptr(), workspace.numel(), _stream_of(cache.device)), "kv_decode")
 
 
 def kv_evict(cache: KvCache, weight: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, new_table: torch.Tensor, keep: int,
@@ -568,18 +587,12 @@ def kv_evict(cache: KvCache, weight: torch.Tensor, page_table: torch.Tensor, len
     must not be pages of page_table; index int32[n_seqs, n_heads, keep], new_weight float32[n_seqs, n_heads, >= keep] and new_lengths
     int32[n_seqs] receive which, their weights, and how many."""
     n = lengths.numel()
-    _here(cache.device)
-    for t, name in ((page_table, "page_table"), (new_table, "new_table")):
-        if t.dim() != 2 or t.shape[0] != n:
-            raise ValueError("%s must have one row per sequence" % name)
-    for t, name in ((page_table, "page_table"), (new_table, "new_table"), (lengths, "lengths"), (index, "index"), (new_lengths, "new_lengths")):
-        _on(t, cache.device, name)
-    if new_lengths.numel() != n or tuple(index.shape) != (n, cache.n_heads, keep):
-        raise ValueError("new_lengths must be [n_seqs] and index [n_seqs, n_heads, keep]")
-    table, stride = _table(page_table, "page_table")
-    fresh, fresh_stride = _table(new_table, "new_table")
-    w, ws = _weight(weight, cache, n, page_table.shape[1] * cache.page_size, "weight")
+    table, stride, max_pages = _pages(page_table, cache, n, "page_table")
+    fresh, fresh_stride, new_pages = _pages(new_table, cache, n, "new_table")
+    if tuple(index.shape) != (n, cache.n_heads, keep):
+        raise ValueError("index must be [n_seqs, n_heads, keep]")
+    w, ws = _weight(weight, cache, n, max_pages * cache.page_size, "weight")
     nw, nws = _weight(new_weight, cache, n, keep, "new_weight")
-    _check(_lib.kv_evict(cache.c, w, ws, n, table, stride, page_table.shape[1], _dev(lengths, torch.int32, "lengths"), fresh, fresh_stride,
-                         new_table.shape[1], int(keep), int(sinks), int(recent), _dev(index, torch.int32, "index"), nw, nws,
-                         new_weight.shape[2], _dev(new_lengths, torch.int32, "new_lengths"), _stream()), "kv_evict")
+    _check(_lib.kv_evict(cache.p, w, ws, n, table, stride, max_pages, _ints(lengths, cache, n, "lengths"), fresh, fresh_stride, new_pages, keep,
+                         sinks, recent, _ints(index, cache, n * cache.n_heads * keep, "index"), nw, nws, new_weight.shape[2],
+                         _ints(new_lengths, cache, n, "new_lengths"), _stream_of(cache.device)), "kv_evict")

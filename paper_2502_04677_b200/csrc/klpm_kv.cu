@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+#include <cooperative_groups.h>
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -999,100 +1000,198 @@ __device__ __forceinline__ unsigned evict_key(const EvictArgs& A, int32_t b, int
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-#define KLPM_EVICT_THREADS 1024
-// One CTA per (sequence, cache head): the key of the last token that is kept is found 8 bits at a time, then the kept
-// tokens are numbered in order of position.
-__global__ void __launch_bounds__(KLPM_EVICT_THREADS) evict_select_kernel(const EvictArgs A) {
-    __shared__ int32_t hist[256];
-    __shared__ int32_t warp_sum[32];
-    __shared__ int32_t s_bin, s_above, s_total;
+// The kept tokens of a row (sequence, cache head), in order of position.  The key of the last one is found 11, 11 and 10 bits at a
+// time from histograms; then everybody counts what lies before its part.  A row belongs to a cluster of CTAs that see each other's
+// histograms through distributed shared memory, a contiguous part each, so that few long rows use many SMs.  HELD: the keys of a CTA's
+// part stay in shared memory (4 bytes a token); beyond that they are made again from the weights for each pass.
+#define KLPM_EVICT_BINS 2048
+#define KLPM_EVICT_HELD 49152          // keys a CTA holds (192 KB)
+struct EvictShared {
+    int32_t hist[3][KLPM_EVICT_BINS];
+    int32_t warp_sum[32], warp_eq[32];
+    int32_t bin, above, count, total;
+    int32_t gt, eq;
+};
+
+template <int T, bool HELD>
+__global__ void __launch_bounds__(T) evict_select_kernel(const EvictArgs A, int32_t ctas) {
+    constexpr int WARPS = T / 32, PER = KLPM_EVICT_BINS / T;
+    extern __shared__ __align__(16) unsigned s_key[];
+    __shared__ EvictShared S;
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int32_t b = blockIdx.x / A.c.n_heads, g = blockIdx.x % A.c.n_heads;
+    const int32_t rank = blockIdx.x % ctas, row = blockIdx.x / ctas;
+    const int32_t b = row / A.c.n_heads, g = row % A.c.n_heads;
     int32_t n = __ldg(A.len + b);
     n = n < 0 ? 0 : n > A.max_tokens ? A.max_tokens : n;
-    int32_t* index = A.index + (int64_t)blockIdx.x * A.keep;
+    const int32_t part = ((n + ctas - 1) / ctas + 31) & ~31;
+    const int32_t t0 = min((long long)rank * part, (long long)n), t1 = min(t0 + part, n);
+    int32_t* index = A.index + (int64_t)row * A.keep;
+    const float* w = A.weight + b * A.ws[0] + g * A.ws[1];
     float* nw = A.new_weight + b * A.nws[0] + g * A.nws[1];
-    // how many there are
-    int32_t mine = 0;
-    for (int32_t t = tid; t < n; t += KLPM_EVICT_THREADS) mine += evict_key(A, b, g, n, t) != 0u;
-    mine = __reduce_add_sync(FULL_MASK, mine);
-    if (lane == 0) warp_sum[warp] = mine;
+    for (int i = tid; i < 3 * KLPM_EVICT_BINS; i += T) (&S.hist[0][0])[i] = 0;
     __syncthreads();
-    if (warp == 0) {
-        const int32_t v = __reduce_add_sync(FULL_MASK, warp_sum[lane]);
-        if (lane == 0) s_total = v;
-    }
-    __syncthreads();
-    const int32_t K = min(A.keep, s_total);
-    unsigned prefix = 0, mask = 0;
-    int32_t want = K;                              // how many of those with this prefix are kept
-    for (int shift = 24; shift >= 0 && K > 0; shift -= 8) {
-        for (int i = tid; i < 256; i += KLPM_EVICT_THREADS) hist[i] = 0;
-        __syncthreads();
-        for (int32_t t = tid; t < n; t += KLPM_EVICT_THREADS) {
-            const unsigned k = evict_key(A, b, g, n, t);
-            if (k != 0u && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
-        }
-        __syncthreads();
-        if (tid == 0) {
-            int32_t above = 0;
-            int bin = 255;
-            for (; bin > 0 && above + hist[bin] < want; --bin) above += hist[bin];
-            s_bin = bin; s_above = above;
-        }
-        __syncthreads();
-        want -= s_above;
-        prefix |= (unsigned)s_bin << shift;
-        mask |= 255u << shift;
-        __syncthreads();
-    }
-    int32_t gt0 = 0, eq0 = 0;
-    for (int32_t base = 0; base < n && K > 0; base += KLPM_EVICT_THREADS) {
-        const int32_t t = base + tid;
+    for (int32_t t = t0 + tid; t < t1; t += T) {
         const unsigned k = evict_key(A, b, g, n, t);
-        const bool gt = k > prefix, eq = k == prefix;
-        const unsigned bg = __ballot_sync(FULL_MASK, gt), be = __ballot_sync(FULL_MASK, eq), below = (1u << lane) - 1;
-        if (lane == 0) warp_sum[warp] = __popc(bg) | __popc(be) << 16;
-        __syncthreads();
-        int32_t before = 0, all = 0;
-        for (int w = 0; w < 32; ++w) { const int32_t v = warp_sum[w]; if (w < warp) before += v; all += v; }
-        const int32_t gts = gt0 + (before & 0xffff) + __popc(bg & below), eqs = eq0 + (before >> 16) + __popc(be & below);
-        if (gt || (eq && eqs < want)) {
-            const int32_t j = gts + min(eqs, want);
-            index[j] = t;
-            nw[j] = __ldg(A.weight + b * A.ws[0] + g * A.ws[1] + t);
-        }
-        gt0 += all & 0xffff;
-        eq0 += all >> 16;
-        __syncthreads();
+        if (HELD) s_key[t - t0] = k;
+        if (k) atomicAdd(&S.hist[0][k >> 21], 1);
     }
-    for (int32_t j = K + tid; j < A.keep; j += KLPM_EVICT_THREADS) index[j] = -1;
-    for (int32_t j = K + tid; j < A.new_len; j += KLPM_EVICT_THREADS) nw[j] = 0.0f;
-    if (g == 0 && tid == 0) A.new_lengths[b] = K;
+    auto key = [&](int32_t t) -> unsigned { return t >= t1 ? 0u : HELD ? s_key[t - t0] : evict_key(A, b, g, n, t); };
+    unsigned limit = 0;                        // kept: keys above it, and the first `want` that equal it
+    int32_t want = 0, K = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        if (pass) {
+            const int up = pass == 1 ? 21 : 10;
+            for (int32_t t = t0 + tid; t < t1; t += T) {
+                const unsigned k = key(t);
+                if (k && (k >> up) == (limit >> up)) atomicAdd(&S.hist[pass][(k >> shift) & (pass == 1 ? 2047 : 1023)], 1);
+            }
+        }
+        cluster.sync();
+        // bins from the top: thread 0 has the highest
+        int32_t c[PER], mine = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int bin = KLPM_EVICT_BINS - 1 - (tid * PER + i);
+            int32_t v = 0;
+            for (int r = 0; r < ctas; ++r) v += cluster.map_shared_rank(&S.hist[pass][0], r)[bin];
+            c[i] = v;
+            mine += v;
+        }
+        int32_t upto = mine;
+        for (int d = 1; d < 32; d <<= 1) {
+            const int32_t v = __shfl_up_sync(FULL_MASK, upto, d);
+            if (lane >= d) upto += v;
+        }
+        if (lane == 31) S.warp_sum[warp] = upto;
+        __syncthreads();
+        int32_t total = 0;
+        for (int i = 0; i < WARPS; ++i) {
+            if (i < warp) upto += S.warp_sum[i];
+            total += S.warp_sum[i];
+        }
+        if (pass == 0) {
+            K = min(A.keep, total);
+            want = K;
+            if (K == total) { want = 0; break; }            // everything that is there is kept: keys above 0
+        }
+        int32_t above = upto - mine;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (above < want && want <= above + c[i]) { S.bin = KLPM_EVICT_BINS - 1 - (tid * PER + i); S.above = above; S.count = c[i]; }
+            above += c[i];
+        }
+        __syncthreads();
+        limit |= (unsigned)S.bin << shift;
+        want -= S.above;
+        const bool all = S.count == want;
+        __syncthreads();
+        if (all) { limit = limit ? limit - 1 : 0u; want = 0; break; }      // the whole bin is kept
+    }
+    // what lies before: in the warps and the CTAs with earlier tokens
+    const int32_t per_warp = (part / 32 + WARPS - 1) / WARPS * 32;
+    const int32_t a0 = min((long long)t0 + (long long)warp * per_warp, (long long)t1), a1 = min(a0 + per_warp, t1);
+    int32_t gts = 0, eqs = 0;
+    if (K > 0)
+        for (int32_t t = a0; t < a1; t += 32) {
+            const unsigned k = t + lane < a1 ? key(t + lane) : 0u;
+            gts += __popc(__ballot_sync(FULL_MASK, k > limit));
+            eqs += __popc(__ballot_sync(FULL_MASK, k == limit && k));
+        }
+    __syncthreads();
+    if (lane == 0) { S.warp_sum[warp] = gts; S.warp_eq[warp] = eqs; }
+    __syncthreads();
+    gts = eqs = 0;
+    int32_t all_gt = 0, all_eq = 0;
+    for (int i = 0; i < WARPS; ++i) {
+        if (i < warp) { gts += S.warp_sum[i]; eqs += S.warp_eq[i]; }
+        all_gt += S.warp_sum[i]; all_eq += S.warp_eq[i];
+    }
+    if (tid == 0) { S.gt = all_gt; S.eq = all_eq; }
+    cluster.sync();
+    for (int r = 0; r < rank; ++r) { gts += *cluster.map_shared_rank(&S.gt, r); eqs += *cluster.map_shared_rank(&S.eq, r); }
+    cluster.sync();                             // nobody leaves while its shared memory is read
+    if (K > 0)
+        for (int32_t t = a0; t < a1; t += 32) {
+            const unsigned k = t + lane < a1 ? key(t + lane) : 0u;
+            const bool gt = k > limit, eq = k == limit && k;
+            const unsigned bg = __ballot_sync(FULL_MASK, gt), be = __ballot_sync(FULL_MASK, eq), below = (1u << lane) - 1;
+            const int32_t e = eqs + __popc(be & below);
+            if (gt || (eq && e < want)) {
+                const int32_t j = gts + __popc(bg & below) + min(e, want);
+                index[j] = t + lane;
+                nw[j] = __ldg(w + t + lane);
+            }
+            gts += __popc(bg);
+            eqs += __popc(be);
+        }
+    for (int32_t j = K + rank * T + tid; j < A.keep; j += ctas * T) index[j] = -1;
+    for (int32_t j = K + rank * T + tid; j < A.new_len; j += ctas * T) nw[j] = 0.0f;
+    if (g == 0 && rank == 0 && tid == 0) A.new_lengths[b] = K;
 }
 
-// 16 bytes of a kept row per thread, keys and values.
+// The kept rows, keys and values: a warp looks up ROWS of them, one per lane, then copies them 16 bytes a lane, eight loads in flight.
+template <int ROWS>
 __global__ void __launch_bounds__(256) evict_copy_kernel(const EvictArgs A) {
-    const int32_t chunks = A.row_bytes / 16;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int32_t x = (int32_t)(id % chunks);
-    const int64_t row = id / chunks;
-    const int32_t g = (int32_t)(row % A.c.n_heads), b = blockIdx.y;
-    const int64_t j = row / A.c.n_heads;
-    if (j >= A.keep) return;
-    const int32_t t = A.index[((int64_t)b * A.c.n_heads + g) * A.keep + j];
-    if (t < 0) return;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const int64_t id = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int32_t g = (int32_t)(id % A.c.n_heads), b = blockIdx.y;
+    const int64_t j0 = id / A.c.n_heads * ROWS;
+    if (j0 >= A.keep) return;
+    const int64_t j = j0 + lane;
     const int32_t in_page = (1 << A.c.page_shift) - 1;
-    const int32_t from = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
-    const int32_t to = __ldg(A.new_table + b * A.new_stride + (j >> A.c.page_shift));
-    if ((unsigned)from >= (unsigned)A.c.n_pages || (unsigned)to >= (unsigned)A.c.n_pages) return;
-    const int64_t sk = from * A.c.ks[0] + (t & in_page) * A.c.ks[1] + g * A.c.ks[2] + x * 16;
-    const int64_t dk = to * A.c.ks[0] + (j & in_page) * A.c.ks[1] + g * A.c.ks[2] + x * 16;
-    const int64_t sv = from * A.c.vs[0] + (t & in_page) * A.c.vs[1] + g * A.c.vs[2] + x * 16;
-    const int64_t dv = to * A.c.vs[0] + (j & in_page) * A.c.vs[1] + g * A.c.vs[2] + x * 16;
-    const int4 a = *reinterpret_cast<const int4*>(A.c.k + sk), c = *reinterpret_cast<const int4*>(A.c.v + sv);
-    *reinterpret_cast<int4*>(A.c.k + dk) = a;
-    *reinterpret_cast<int4*>(A.c.v + dv) = c;
+    int64_t sk = -1, dk = 0, sv = 0, dv = 0;      // sk < 0: nothing to copy
+    if (lane < ROWS && j < A.keep) {
+        const int32_t t = A.index[((int64_t)b * A.c.n_heads + g) * A.keep + j];
+        if (t >= 0) {
+            const int32_t from = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
+            const int32_t to = __ldg(A.new_table + b * A.new_stride + (j >> A.c.page_shift));
+            if ((unsigned)from < (unsigned)A.c.n_pages && (unsigned)to < (unsigned)A.c.n_pages) {
+                sk = from * A.c.ks[0] + (t & in_page) * A.c.ks[1] + g * A.c.ks[2];
+                sv = from * A.c.vs[0] + (t & in_page) * A.c.vs[1] + g * A.c.vs[2];
+                dk = to * A.c.ks[0] + (j & in_page) * A.c.ks[1] + g * A.c.ks[2];
+                dv = to * A.c.vs[0] + (j & in_page) * A.c.vs[1] + g * A.c.vs[2];
+            }
+        }
+    }
+    const unsigned slots = A.row_bytes / 8;        // 16-byte pieces of a row's key and value together, at most 64
+    const unsigned magic = (1u << 20) / slots + 1; // e * magic >> 20 = e / slots for e < 2^20 / slots
+    constexpr int DEEP = 8;
+    for (unsigned e0 = 0; e0 < ROWS * slots; e0 += 32 * DEEP) {
+        int4 v[DEEP];
+        char* to[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            const unsigned e = e0 + i * 32 + lane;
+            const unsigned r = e * magic >> 20, x = e - r * slots;
+            const int64_t s0 = __shfl_sync(FULL_MASK, sk, r & 31), s1 = __shfl_sync(FULL_MASK, sv, r & 31);
+            const int64_t d0 = __shfl_sync(FULL_MASK, dk, r & 31), d1 = __shfl_sync(FULL_MASK, dv, r & 31);
+            const bool value = x >= slots / 2;
+            to[i] = nullptr;
+            if (r < ROWS && s0 >= 0) {
+                to[i] = value ? A.c.v + d1 + (x - slots / 2) * 16 : A.c.k + d0 + x * 16;
+                v[i] = *reinterpret_cast<const int4*>(value ? A.c.v + s1 + (x - slots / 2) * 16 : A.c.k + s0 + x * 16);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+            if (to[i]) *reinterpret_cast<int4*>(to[i]) = v[i];
+    }
+}
+
+template <int T, bool HELD> rt_status launch_select(const EvictArgs& A, int64_t rows, int ctas, size_t smem, cudaStream_t s) {
+    CK(cudaFuncSetAttribute(evict_select_kernel<T, HELD>, cudaFuncAttributeMaxDynamicSharedMemorySize, KLPM_EVICT_HELD * 4));
+    cudaLaunchConfig_t c = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = ctas; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    c.gridDim = dim3((unsigned)(rows * ctas)); c.blockDim = dim3(T); c.dynamicSmemBytes = smem; c.stream = s; c.attrs = at; c.numAttrs = 1;
+    CK(cudaLaunchKernelEx(&c, evict_select_kernel<T, HELD>, A, (int32_t)ctas));
+    return RT_OK;
 }
 
 }  // namespace
@@ -1235,13 +1334,20 @@ rt_status kv_evict(const kv_cache* cache, const float* d_weight, const int64_t* 
     A.new_lengths = d_new_lengths;
     cudaStream_t s = (cudaStream_t)stream;
     const int64_t rows = (int64_t)n_seqs * cache->n_heads;
-    const int64_t blocks = ((int64_t)keep * cache->n_heads * (A.row_bytes / 16) + 255) / 256;
-    if (rows > 0x7fffffffLL || blocks > 0x7fffffffLL) return RT_ERR_TOO_LARGE;
-    evict_select_kernel<<<(unsigned)rows, KLPM_EVICT_THREADS, 0, s>>>(A);
-    CK(cudaGetLastError());
-    evict_copy_kernel<<<dim3((unsigned)blocks, (unsigned)n_seqs), 256, 0, s>>>(A);
-    CK(cudaGetLastError());
-    return RT_OK;
+    // CTAs per row: as many as it takes to hold the keys, and more of them while rows leave SMs idle
+    int ctas = 1;
+    while (ctas < 8 && ((int64_t)ctas * KLPM_EVICT_HELD < A.max_tokens || (rows * ctas * 2 <= KLPM_SMS && A.max_tokens / ctas > 4096))) ctas *= 2;
+    const int64_t part = ((A.max_tokens + ctas - 1) / ctas + 31) & ~31LL;
+    // rows of a warp of the copy: 8 while that leaves every warp of the GPU at most one turn
+    const int rpw = rows * keep <= (int64_t)KLPM_SMS * 64 * 8 ? 8 : 32;
+    const int64_t blocks = ((int64_t)((keep + rpw - 1) / rpw) * cache->n_heads + 7) / 8;
+    if (rows * ctas > 0x7fffffffLL || blocks > 0x7fffffffLL) return RT_ERR_TOO_LARGE;
+    if (part > KLPM_EVICT_HELD) st = launch_select<1024, false>(A, rows, ctas, 0, s);
+    else if (part > 2048) st = launch_select<1024, true>(A, rows, ctas, (size_t)part * 4, s);
+    else st = launch_select<256, true>(A, rows, ctas, (size_t)part * 4, s);
+    if (st) return st;
+    const dim3 grid((unsigned)blocks, (unsigned)n_seqs);
+    return rpw == 8 ? launch_after(evict_copy_kernel<8>, grid, 256, s, A) : launch_after(evict_copy_kernel<32>, grid, 256, s, A);
 }
 
 }  // extern "C"

@@ -520,6 +520,7 @@ EVICT = [
     ([5000], 37, 0, 0, 2, 64, 64, "nhd", E4),
     ([20_011, 9000], 4099, 16, 1000, 1, 64, 16, "hnd", HF),
     ([70_001], 65_000, 0, 1, 2, 16, 32, "nhd", E4),
+    ([400_001, 37, 3000], 5000, 3, 100, 1, 16, 64, "nhd", E4),
 ]
 
 

@@ -36,22 +36,28 @@ BAD_CACHES = [dict(k=None), dict(v=None), dict(dtype=0), dict(dtype=7), dict(n_p
 LARGE_CACHES = [dict(head_dim=320), dict(page_size=1 << 17), dict(n_pages=1 << 30)]
 
 
+def at(x):
+    return ctypes.addressof(x) if x is not None else None
+
+
 def decode(K, c, q=None, out=None, n=3, table=P, table_stride=8, max_pages=8, lengths=P, scale=0.1, window=0, lse=None, weight=None, ws=None,
            work=P, work_bytes=1 << 40):
     ws = (ctypes.c_int64 * 2)(*ws) if ws else None
-    return K.lib().kv_decode(c, q or rows(K, 4), out or rows(K, 4, data=2 * P), n, table, table_stride, max_pages, lengths, scale, window, lse, weight,
-                             ws, work, work_bytes, None)
+    q, out = q or rows(K, 4), out or rows(K, 4, data=2 * P)
+    return K.lib().kv_decode(at(c), at(q), at(out), n, table, table_stride, max_pages, lengths, scale, window, lse, weight,
+                             at(ws), work, work_bytes, None)
 
 
 def append(K, c, rope=None, pos=P, slots=P, n=3, q=None, q_out=None, k=None, v=None):
-    return K.lib().kv_rope_append(c, rope, pos, slots, n, q, q_out, k or rows(K, 2), v or rows(K, 2), None)
+    keep = [k or rows(K, 2), v or rows(K, 2)]
+    return K.lib().kv_rope_append(at(c), at(rope), pos, slots, n, at(q), at(q_out), at(keep[0]), at(keep[1]), None)
 
 
 def evict(K, c, weight=P, ws=(256, 128), n=3, table=P, table_stride=8, max_pages=8, lengths=P, new=P, new_stride=2, new_pages=2, keep=20, sinks=2,
           recent=4, index=P, nw=P, nws=(256, 128), new_len=128, new_lengths=P):
-    s = lambda x: (ctypes.c_int64 * 2)(*x) if x else None
-    return K.lib().kv_evict(c, weight, s(ws), n, table, table_stride, max_pages, lengths, new, new_stride, new_pages, keep, sinks, recent, index, nw,
-                            s(nws), new_len, new_lengths, None)
+    a, b = ((ctypes.c_int64 * 2)(*x) if x else None for x in (ws, nws))
+    return K.lib().kv_evict(at(c), weight, at(a), n, table, table_stride, max_pages, lengths, new, new_stride, new_pages, keep, sinks, recent, index, nw,
+                            at(b), new_len, new_lengths, None)
 
 
 def test_every_declared_call_is_exported(K):
@@ -68,7 +74,7 @@ def test_bad_caches(K, change):
     assert decode(K, c) == K.RT_ERR_INVALID
     assert append(K, c) == K.RT_ERR_INVALID
     assert evict(K, c) == K.RT_ERR_INVALID
-    assert K.lib().kv_decode_workspace(c, 3, 4, 8, 0) == K.RT_ERR_INVALID
+    assert K.lib().kv_decode_workspace(at(c), 3, 4, 8, 0) == K.RT_ERR_INVALID
 
 
 @pytest.mark.parametrize("change", LARGE_CACHES, ids=str)
@@ -92,9 +98,9 @@ def test_decode_refusals(K):
     assert decode(K, c, max_pages=1 << 27, table_stride=1 << 27) == K.RT_ERR_TOO_LARGE
     assert decode(K, c, n=1 << 17) == K.RT_ERR_TOO_LARGE
     assert decode(K, c, n=0) == K.RT_OK
-    need = K.lib().kv_decode_workspace(c, 3, 4, 8, 1)
+    need = K.lib().kv_decode_workspace(at(c), 3, 4, 8, 1)
     assert need > 0 and decode(K, c, weight=P, ws=(256, 128), work_bytes=need - 1) == K.RT_ERR_INVALID
-    assert K.lib().kv_decode_workspace(c, -1, 4, 8, 0) == K.lib().kv_decode_workspace(c, 3, 3, 8, 0) == K.RT_ERR_INVALID
+    assert K.lib().kv_decode_workspace(at(c), -1, 4, 8, 0) == K.lib().kv_decode_workspace(at(c), 3, 3, 8, 0) == K.RT_ERR_INVALID
 
 
 def test_append_refusals(K):
