@@ -262,16 +262,18 @@ template <int TX, int TC> void launch_append(const AppendArgs& A, bool vec, unsi
 //
 // The floor is one read of the cache's rows (512 B per token and cache head at 128 elements of 16 bits, against a few flops per
 // byte), so everything is laid out for loads in flight:
-//   - The query heads of a cache head go through the tensor cores together (mma.sync, 16 x 8 x 16): a tile of keys is read
-//     once for all of them.  tcgen05 has nothing to give here: its tiles would hold 128 rows of heads where there are 1 to 16.
-//   - A warp works alone: its tiles (16 or 32 tokens) come through a ring of its own in shared memory (cp.async, 16 bytes a lane, 3
-//     stages of 8 KB), with its own m and sums.  No barrier in the loop.
+//   - The query heads of a cache head go through the tensor cores together (mma.sync, 16 x 8 x 16): a tile of keys is read once for
+//     all of them.  Tokens, then elements of the values, take the 16 rows of the operand that comes from shared memory, 8 heads the
+//     8 columns.  tcgen05 has nothing to give here: its tiles would hold 128 rows for a few flops per byte that is read anyway.
+//   - A warp works alone: its half tiles (4 KB of keys, then of values, 16 or 32 tokens) come through a ring of its own in shared
+//     memory (cp.async, 16 bytes a lane), with its own m and sums.  No barrier in the loop.  16 warps on an SM hide what the
+//     dependent steps of one take, and keep 128 KB in flight.
 //   - All tiles of the batch, in the order (sequence, unit, tile), are cut into equal spans, one per warp of a grid that fills the
 //     GPU once: ragged lengths leave no warp with more than another.  A row that is cut is joined by decode_join_kernel.
 //     A unit is a cache head and up to 8 NT of its query heads.
-//   - Probabilities enter the second product as the sum of two 16-bit numbers (16 bits of precision or more).  With up to 8
-//     heads in a 16-row operand the second one takes the 8 free rows: it costs nothing.  f16 probabilities are scaled by 2^15 so that
-//     small ones keep their bits.  A bf16 query next to an 8-bit cache is split into two f16 numbers in the same way.
+//   - Probabilities enter the second product as the sum of two 16-bit numbers (16 bits of precision or more), whose products go to the same
+//     sums.  f16 probabilities are scaled by 2^15 so that small ones keep their bits.  A bf16 query next to an 8-bit cache
+//     is split into two f16 numbers in the same way.
 // ------------------------------------------------------------------------------------------------
 struct DecodeArgs {
     CacheDev c;
@@ -286,7 +288,7 @@ struct DecodeArgs {
     int64_t ws[2];
     // workspace
     long long* tiles_before;           // [n_seqs + 1] tiles of the sequences before
-    float* lse2;                       // [n_seqs, q heads] base-2 logarithm of the softmax's sum (with weight only)
+    float* lse2;                       // [n_seqs, q heads] base-2 logarithm of the softmax's sum
     float* part;                       // [warps][2][8 NT][2 + DP]: m, sum, output of the two rows that a warp may share with others
     float* score;                      // [n_seqs, q heads, score_len] (with weight only)
     int64_t score_len;
@@ -305,14 +307,15 @@ template <int TQ_, int TC_, int DP_, int NT_> struct Dec {
     static constexpr int ROW = DP * (E8 ? 1 : 2);              // bytes of a row in shared memory
     static constexpr int CH = ROW / 16;
     static constexpr int TT = (E8 ? DP <= 128 : DP <= 64) ? 32 : 16;
-    static constexpr int TILE = TT * ROW, STAGE = 2 * TILE;
-    static constexpr int STAGES = STAGE <= 4096 ? 6 : 3;
-    static constexpr int WARP_SMEM = STAGES * STAGE;
+    static constexpr int TILE = TT * ROW;                      // bytes of a half tile: keys or values
+    static constexpr int CTAS = DP > 128 || NT > 1 ? 2 : QLO ? 3 : 4;      // per SM: what the registers leave room for
+    static constexpr int FIT = 192 * 1024 / (CTAS * KLPM_DECODE_WARPS * TILE);
+    static constexpr int RING = FIT < 6 ? FIT : 6;             // half tiles
+    static constexpr int WARP_SMEM = RING * TILE;
     static constexpr int SMEM = KLPM_DECODE_WARPS * WARP_SMEM;
-    static constexpr int CTAS = SMEM <= 100 * 1024 ? 2 : 1;    // per SM
     static constexpr int HEADS = 8 * NT;
     static constexpr int PART = HEADS * (2 + DP);
-    static constexpr int QF = QLO ? NT : 1;                    // query operands
+    static constexpr int QF = QLO ? 2 : 1;                     // numbers that a query element is the sum of
 };
 
 __device__ __forceinline__ void token_range(const DecodeArgs& A, int32_t b, int32_t* lo, int32_t* hi) {
@@ -362,6 +365,11 @@ template <bool HALF> __device__ __forceinline__ void mma16816(float (&c)[4], uin
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {          // of 16-bit elements, lane 4r + j holding columns 2j, 2j+1 of row r
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
 __device__ __forceinline__ uint32_t e4m3_to_f16(uint32_t two) {           // exact; the low 16 bits hold two values
     uint32_t r;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));
@@ -380,12 +388,6 @@ template <bool HALF> __device__ __forceinline__ void split2(float x, float y, ui
         const __nv_bfloat162 l = __floats2bfloat162_rn(x - f.x, y - f.y);
         *hi = *reinterpret_cast<const uint32_t*>(&h); *lo = *reinterpret_cast<const uint32_t*>(&l);
     }
-}
-// The two halves of an output.  An infinite value times the second half of a probability, which may be 0 or negative, is no number: the
-// first half alone then says what the sum is.
-__device__ __forceinline__ float both(float hi, float lo) {
-    const float x = hi + lo;
-    return x == x ? x : hi;
 }
 __device__ __forceinline__ float exp2_fast(float x) {        // 2 ulp; 2^-inf = 0
     float r;
@@ -409,10 +411,10 @@ template <class X> __device__ __forceinline__ int q_element(int ks, int j, int p
     if constexpr (X::E8) return (ks >> 2) * 64 + j * 16 + (ks & 3) * 4 + part * 2;
     else return ks * 16 + j * 2 + part * 8;
 }
-// The element that column 2j + e of output tile x stands for.
-template <class X> __device__ __forceinline__ int out_element(int x, int j, int e) {
-    if constexpr (X::E8) return (2 * j + e) * (X::DP / 8) + x;
-    else return x * 8 + 2 * j + e;
+// The element that row r + 8e of output tile x stands for.
+template <class X> __device__ __forceinline__ int out_element(int x, int r, int e) {
+    if constexpr (X::E8) return r * (X::DP / 8) + 2 * x + e;
+    else return x * 16 + r + 8 * e;
 }
 
 template <class X> struct Cursor {       // a tile of the batch
@@ -437,19 +439,22 @@ template <class X> struct Cursor {       // a tile of the batch
 };
 
 template <class X>
-__global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel(const DecodeArgs A) {
+__global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel(const __grid_constant__ DecodeArgs A) {
     using Q = typename Elem<X::TQ>::T;
-    constexpr int TT = X::TT, KS = X::DP / 16, VN = X::DP / 8, TN = TT / 8, NT = X::NT;
+    constexpr int TT = X::TT, KS = X::DP / 16, TN = TT / 16, NT = X::NT, RING = X::RING;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ long long s_sum[KLPM_DECODE_WARPS];
     __shared__ int32_t s_b[KLPM_DECODE_WARPS];
     __shared__ long long s_rem[KLPM_DECODE_WARPS];
+    __shared__ unsigned s_there[KLPM_DECODE_WARPS][8];         // which tokens of the tiles on their way are there
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    for (int i = tid; i < X::SMEM / 16; i += KLPM_DECODE_WARPS * 32) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);  // elements behind dim stay 0
+    const int32_t chunks = A.c.dim * (X::E8 ? 1 : 2) / 16;
+    if (chunks < X::CH)                                       // elements behind dim stay 0
+        for (int i = tid; i < X::SMEM / 16; i += KLPM_DECODE_WARPS * 32) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
     // where each warp starts: every CTA adds up the tiles of all sequences
     const int32_t per = (A.n_seqs + KLPM_DECODE_WARPS * 32 - 1) / (KLPM_DECODE_WARPS * 32);
-    const int32_t b0 = min((int64_t)tid * per, (int64_t)A.n_seqs), b1 = min((int64_t)b0 + per, (int64_t)A.n_seqs);
+    const int32_t b0 = min(tid * per, A.n_seqs), b1 = min(b0 + per, A.n_seqs);
     long long mine = 0;
     int32_t first;
     for (int32_t b = b0; b < b1; ++b) mine += tiles_of<TT>(A, b, &first);
@@ -505,59 +510,89 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
 
     const uint32_t ring = smem_addr(smem) + warp * X::WARP_SMEM;
     const int32_t in_page = (1 << A.c.page_shift) - 1;
-    const int32_t chunks = A.c.dim * (X::E8 ? 1 : 2) / 16;
     const int my_row = lane / X::CH % TT, my_ch = lane % X::CH;
-    // the page of token `lane` of the tile that is loaded next; -1: nothing there
+    // the page of token `lane` of the tile at ci; -1: nothing there
     auto page_of = [&]() -> int32_t {
         const int32_t t = ci.tile * TT + lane;
         if (lane >= TT || t < ci.lo || t >= ci.hi) return -1;
         const int32_t p = __ldg(A.table + ci.b * A.table_stride + (t >> A.c.page_shift));
         return (unsigned)p < (unsigned)A.c.n_pages ? p : -1;
     };
-    int32_t page = page_of();
-    int slot_in = 0;
-    auto load_tile = [&]() -> unsigned {                      // returns which tokens are there
-        unsigned there = 0;
-        if (to_load > 0) {
-            there = __ballot_sync(FULL_MASK, page >= 0);
-            const uint32_t dk = ring + slot_in * X::STAGE, dv = dk + X::TILE;
-            const int32_t g = ci.u / A.head_tiles;
-            const char* kb = A.c.k + g * A.c.ks[2] + my_ch * 16;
-            const char* vb = A.c.v + g * A.c.vs[2] + my_ch * 16;
-            constexpr int RPI = 32 / X::CH;                   // rows of one instruction
+    int32_t page_next = page_of(), page = -1, at = 0, g_now = 0;           // (at: the lane's token's place in its page)
+    int slot_in = 0, tile_in = 0;
+    auto copy_rows = [&](auto value) {
+        constexpr bool VALUE = decltype(value)::value;
+        constexpr int RPI = 32 / X::CH;                       // rows of one instruction
+        const int64_t s0 = VALUE ? A.c.vs[0] : A.c.ks[0], s1 = VALUE ? A.c.vs[1] : A.c.ks[1];
+        const char* base = (VALUE ? A.c.v : A.c.k) + g_now * (VALUE ? A.c.vs[2] : A.c.ks[2]) + my_ch * 16;
+        const uint32_t to = ring + slot_in * X::TILE;
+        if (A.c.page_shift >= (TT == 32 ? 5 : 4) && __all_sync(FULL_MASK, lane >= TT || page >= 0)) {
+            // the whole tile lies in one page
+            const char* p = base + page * s0 + (at - lane + my_row) * s1;          // (page and at - lane are the same in all lanes below TT)
+            if constexpr (TT < 32) p = base + __shfl_sync(FULL_MASK, page, 0) * s0 + (__shfl_sync(FULL_MASK, at, 0) + my_row) * s1;
+            if (my_ch < chunks) {
 #pragma unroll
-            for (int i = 0; i < TT / RPI; ++i) {
-                const int r = i * RPI + my_row;
-                const int32_t p = __shfl_sync(FULL_MASK, page, r);
-                const int32_t at = (ci.tile * TT + r) & in_page;
-                const int64_t ok = p < 0 ? 0 : p * A.c.ks[0] + at * A.c.ks[1], ov = p < 0 ? 0 : p * A.c.vs[0] + at * A.c.vs[1];
-                if (my_ch < chunks) {
-                    cp_async16(dk + place<X, false>(r, my_ch) * 16, kb + ok, p < 0 ? 0 : 16);
-                    cp_async16(dv + place<X, true>(r, my_ch) * 16, vb + ov, p < 0 ? 0 : 16);
+                for (int i = 0; i < TT / RPI; ++i) {
+                    cp_async16(to + place<X, VALUE>(i * RPI + my_row, my_ch) * 16, p, 16);
+                    p += RPI * s1;
                 }
             }
-            if (--to_load > 0) {
-                ci.next(A);
-                page = page_of();
+        } else {
+            const int64_t mine = page < 0 ? -1 : page * s0 + at * s1;
+#pragma unroll
+            for (int i = 0; i < TT / RPI; ++i) {
+                const int64_t off = __shfl_sync(FULL_MASK, mine, i * RPI + my_row);
+                if (my_ch < chunks) cp_async16(to + place<X, VALUE>(i * RPI + my_row, my_ch) * 16, off < 0 ? base : base + off, off < 0 ? 0 : 16);
             }
-            if (++slot_in == X::STAGES) slot_in = 0;
+        }
+        if (++slot_in == RING) slot_in = 0;
+    };
+    auto load_keys = [&]() {
+        if (to_load > 0) {
+            page = page_next;
+            at = (ci.tile * TT + lane) & in_page;
+            g_now = ci.u / A.head_tiles;
+            const unsigned there = __ballot_sync(FULL_MASK, page >= 0);
+            if (lane == 0) s_there[warp][tile_in & 7] = there;
+            ++tile_in;
+            if (to_load > 1) {
+                ci.next(A);
+                page_next = page_of();
+            }
+            copy_rows(std::false_type());
         }
         cp_async_commit();
-        return there;
+    };
+    auto load_values = [&]() {
+        if (to_load > 0) {
+            --to_load;
+            copy_rows(std::true_type());
+        }
+        cp_async_commit();
     };
 
     const int r8 = lane >> 2, j = lane & 3;
     const float log2e = 1.4426950408889634f;
-    unsigned there[X::STAGES];
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < X::STAGES - 1; ++i) there[i] = load_tile();
-
-    uint32_t qa[X::QF][KS][(NT == 1 && !X::QLO) ? 2 : 4];
-    float coef[NT], m[NT], l[NT], o[NT][VN][4];
+    // where the lane's rows of an ldmatrix are: chunk c of row r lies at r * ROW + ((c ^ r) & 7 | c & ~7) * 16.  Keys: tokens 0-15, two chunks;
+    // values: tokens 0-7 and 8-15 of two chunks
+    const int kr = lane & 15, kc = lane >> 4, vr = (lane & 7) + ((lane >> 4) << 3), vc = (lane >> 3) & 1;
+    uint32_t qb[X::QF][NT][KS][2];
+    float coef[NT][2], m[NT][2], l[NT][2], o[NT][KS][4];
     bool fresh = true, begun_here = false, first_piece = true;
     int32_t heads = 0;
-    int slot_out = 0;
+    int slot_out = 0, tile_out = 0;
+    auto step = [&]() -> uint32_t {                           // the next half tile has arrived, and the one before it is no longer read
+        cp_async_wait<RING - 2>();
+        __syncwarp();
+        const uint32_t a = ring + slot_out * X::TILE;
+        if (++slot_out == RING) slot_out = 0;
+        return a;
+    };
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i) {
+        if (i & 1) load_values();
+        else load_keys();
+    }
     for (; left > 0; --left) {
         if (fresh) {                                          // a row begins, or the span begins inside one
             fresh = false;
@@ -566,14 +601,16 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
             heads = min(X::HEADS, A.group - h0);
             const char* qp = A.q.p + cc.b * A.q.sr + (int64_t)(g * A.group + h0) * A.q.sh;
 #pragma unroll
-            for (int f = 0; f < X::QF; ++f) {
-                float up = 1.0f;
+            for (int n = 0; n < NT; ++n) {
+                const bool have = n * 8 + r8 < heads;
+                const Q* q = reinterpret_cast<const Q*>(qp + (n * 8 + r8) * A.q.sh);
+                float up = 1.0f, c = A.scale * A.c.k_scale * log2e;
                 if constexpr (X::QLO) {
                     // a power of two brings the largest element next to 2^15: f16 pairs then hold elements down to 2^-39 of it exactly
                     float most = 0.0f;
-                    if (f * 8 + r8 < heads)
+                    if (have)
                         for (int d = j; d < A.c.dim; d += 4) {
-                            const float x = fabsf(to_float(reinterpret_cast<const Q*>(qp + (f * 8 + r8) * A.q.sh)[d]));
+                            const float x = fabsf(to_float(q[d]));
                             if (x < INFINITY) most = fmaxf(most, x);
                         }
                     most = fmaxf(most, __shfl_xor_sync(FULL_MASK, most, 1));
@@ -582,57 +619,45 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
                     if (most > 0.0f) frexpf(most, &e);
                     e = max(-110, min(110, 15 - e));
                     up = ldexpf(1.0f, e);
-                    coef[f] = ldexpf(A.scale * A.c.k_scale * log2e, -e);
+                    c = ldexpf(c, -e);
                 }
+                coef[n][0] = __shfl_sync(FULL_MASK, c, 8 * j);           // of heads 2j and 2j+1
+                coef[n][1] = __shfl_sync(FULL_MASK, c, 8 * j + 4);
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
                     for (int part = 0; part < 2; ++part) {
                         const int d = q_element<X>(ks, j, part);
-                        auto get = [&](int head, int e) -> float {
-                            return head < heads && d + e < A.c.dim ? to_float(reinterpret_cast<const Q*>(qp + head * A.q.sh)[d + e]) : 0.0f;
-                        };
+                        const float x = have && d < A.c.dim ? to_float(q[d]) * up : 0.0f, y = have && d + 1 < A.c.dim ? to_float(q[d + 1]) * up : 0.0f;
+                        uint32_t lo;
+                        split2<X::HALF>(x, y, &qb[0][n][ks][part], &lo);
                         if constexpr (X::QLO) {
-                            const float x = get(f * 8 + r8, 0) * up, y = get(f * 8 + r8, 1) * up;
-                            split2<true>(x, y, &qa[f][ks][part * 2], &qa[f][ks][part * 2 + 1]);
                             // (an infinite element minus itself would be NaN: its second half is 0)
-                            const __half2 h = *reinterpret_cast<const __half2*>(&qa[f][ks][part * 2]);
-                            if (__hisinf(h.x)) qa[f][ks][part * 2 + 1] &= 0xffff0000u;
-                            if (__hisinf(h.y)) qa[f][ks][part * 2 + 1] &= 0x0000ffffu;
-                        } else {
-                            uint32_t lo;
-                            split2<X::HALF>(get(r8, 0), get(r8, 1), &qa[0][ks][NT == 1 ? part : part * 2], &lo);
-                            if constexpr (NT == 2) split2<X::HALF>(get(r8 + 8, 0), get(r8 + 8, 1), &qa[0][ks][part * 2 + 1], &lo);
+                            if (isinf(x)) lo &= 0xffff0000u;
+                            if (isinf(y)) lo &= 0x0000ffffu;
+                            qb[X::QF - 1][n][ks][part] = lo;
                         }
                     }
-            }
-            if constexpr (!X::QLO)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) coef[n] = A.scale * A.c.k_scale * log2e;
+                for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.0f; }
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                m[n] = -INFINITY; l[n] = 0.0f;
-#pragma unroll
-                for (int x = 0; x < VN; ++x) o[n][x][0] = o[n][x][1] = o[n][x][2] = o[n][x][3] = 0.0f;
+                for (int x = 0; x < KS; ++x) o[n][x][0] = o[n][x][1] = o[n][x][2] = o[n][x][3] = 0.0f;
             }
         }
-        cp_async_wait<X::STAGES - 2>();
-        __syncwarp();                                         // everybody's part of this tile is there, and the tile before it is no longer read
-        there[X::STAGES - 1] = load_tile();
-        const uint32_t sk = ring + slot_out * X::STAGE, sv = sk + X::TILE;
-        if (++slot_out == X::STAGES) slot_out = 0;
-        // s = q . k
-        float s[X::QF][TN][4];
+        // s = k . q, tokens x heads
+        const uint32_t sk = step();
+        if constexpr (RING & 1) load_keys();
+        else load_values();
+        float s[NT][TN][4];
 #pragma unroll
-        for (int f = 0; f < X::QF; ++f)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int t = 0; t < TN; ++t) s[f][t][0] = s[f][t][1] = s[f][t][2] = s[f][t][3] = 0.0f;
-        auto qk = [&](int t, int ks, uint32_t b0, uint32_t b1) {
+            for (int t = 0; t < TN; ++t) s[n][t][0] = s[n][t][1] = s[n][t][2] = s[n][t][3] = 0.0f;
+        auto kq = [&](int t, int ks, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-            for (int f = 0; f < X::QF; ++f) {
-                if constexpr (NT == 1 && !X::QLO) mma16816<X::HALF>(s[f][t], qa[f][ks][0], 0u, qa[f][ks][1], 0u, b0, b1);
-                else mma16816<X::HALF>(s[f][t], qa[f][ks][0], qa[f][ks][1], qa[f][ks][2], qa[f][ks][3], b0, b1);
-            }
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int f = 0; f < X::QF; ++f) mma16816<X::HALF>(s[n][t], a0, a1, a2, a3, qb[f][n][ks][0], qb[f][n][ks][1]);
         };
         if constexpr (X::E8) {
 #pragma unroll
@@ -640,75 +665,112 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
                 if (hb * 64 >= A.c.dim) break;
 #pragma unroll
                 for (int t = 0; t < TN; ++t) {
-                    const uint4 v = lds128(sk + place<X, false>(t * 8 + r8, hb * 4 + j) * 16);
-                    qk(t, hb * 4 + 0, e4m3_to_f16(v.x), e4m3_to_f16(v.x >> 16));
-                    qk(t, hb * 4 + 1, e4m3_to_f16(v.y), e4m3_to_f16(v.y >> 16));
-                    qk(t, hb * 4 + 2, e4m3_to_f16(v.z), e4m3_to_f16(v.z >> 16));
-                    qk(t, hb * 4 + 3, e4m3_to_f16(v.w), e4m3_to_f16(v.w >> 16));
+                    const uint4 a = lds128(sk + place<X, false>(t * 16 + r8, hb * 4 + j) * 16), b = lds128(sk + place<X, false>(t * 16 + 8 + r8, hb * 4 + j) * 16);
+                    kq(t, hb * 4 + 0, e4m3_to_f16(a.x), e4m3_to_f16(b.x), e4m3_to_f16(a.x >> 16), e4m3_to_f16(b.x >> 16));
+                    kq(t, hb * 4 + 1, e4m3_to_f16(a.y), e4m3_to_f16(b.y), e4m3_to_f16(a.y >> 16), e4m3_to_f16(b.y >> 16));
+                    kq(t, hb * 4 + 2, e4m3_to_f16(a.z), e4m3_to_f16(b.z), e4m3_to_f16(a.z >> 16), e4m3_to_f16(b.z >> 16));
+                    kq(t, hb * 4 + 3, e4m3_to_f16(a.w), e4m3_to_f16(b.w), e4m3_to_f16(a.w >> 16), e4m3_to_f16(b.w >> 16));
                 }
             }
         } else {
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                if (ks * 16 >= A.c.dim) break;
+            for (int k4 = 0; k4 < KS; k4 += 4) {
+                if (k4 * 16 >= A.c.dim) break;
 #pragma unroll
-                for (int t = 0; t < TN; t += 2) {
-                    uint32_t b[4];          // tokens 0-7 and 8-15 of the pair, elements 0-7 and 8-15 of the step
-                    ldmatrix4(b, sk + place<X, false>(t * 8 + (lane & 7) + ((lane >> 4) << 3), ks * 2 + ((lane >> 3) & 1)) * 16);
-                    qk(t, ks, b[0], b[1]);
-                    qk(t + 1, ks, b[2], b[3]);
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t base = sk + kr * X::ROW + (((2 * k + kc) ^ kr) & 7) * 16;
+#pragma unroll
+                    for (int t = 0; t < TN; ++t) {
+                        uint32_t a[4];          // tokens 0-7 and 8-15 of elements 0-7, then of 8-15
+                        ldmatrix4(a, base + t * 16 * X::ROW + k4 * 32);
+                        kq(t, k4 + k, a[0], a[1], a[2], a[3]);
+                    }
                 }
             }
         }
-        // p = 2^(s - m), in place
-        const unsigned have = there[0];
-        uint32_t pa[NT][TN / 2][4];
+        // p = 2^(s - m): tokens r8 and r8 + 8 of heads 2j and 2j + 1
+        const unsigned have = s_there[warp][tile_out++ & 7];
+        uint32_t ph[NT][TN][2], pl[NT][TN][2];
+        bool grown = false;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float z[TN][2];
-            float top = m[n];
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int t = 0; t < TN; ++t)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float x = X::QLO ? s[n * (X::QF - 1)][t][e] + s[n * (X::QF - 1)][t][e + 2] : s[0][t][n * 2 + e];
-                    x = (have >> (t * 8 + 2 * j + e)) & 1 ? x * coef[n] : -INFINITY;
-                    z[t][e] = x;
-                    top = fmaxf(top, x);
+                for (int i = 0; i < 4; ++i) {
+                    float& z = s[n][t][i];
+                    z *= coef[n][i & 1];
+                    if (have != (TT == 32 ? 0xffffffffu : 0xffffu) && !((have >> (t * 16 + (i >> 1) * 8 + r8)) & 1)) z = -INFINITY;
+                    grown |= z > m[n][i & 1];
                 }
-            if (A.weight && n * 8 + r8 < heads) {
-                const int32_t g = cc.u / A.head_tiles, h = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS + n * 8 + r8;
-                float* row = A.score + ((int64_t)cc.b * A.q.heads + h) * A.score_len + (int64_t)cc.tile * TT + 2 * j;
+        if (A.weight) {
+            const int32_t g = cc.u / A.head_tiles, h0 = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS;
+            float* row = A.score + ((int64_t)cc.b * A.q.heads + h0) * A.score_len + (int64_t)cc.tile * TT + r8;
 #pragma unroll
-                for (int t = 0; t < TN; ++t) *reinterpret_cast<float2*>(row + t * 8) = make_float2(z[t][0], z[t][1]);
-            }
-            top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 2));
-            if (__any_sync(FULL_MASK, top > m[n])) {          // rare after the first tiles
-                const float f = m[n] == -INFINITY ? 0.0f : exp2_fast(m[n] - top);
-                l[n] *= f;
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int x = 0; x < VN; ++x) { o[n][x][0] *= f; o[n][x][1] *= f; o[n][x][2] *= f; o[n][x][3] *= f; }
-                m[n] = top;
-            }
-            const float base = m[n] == -INFINITY ? 0.0f : m[n] - (X::HALF ? 15.0f : 0.0f);
+                for (int t = 0; t < TN; ++t)
 #pragma unroll
-            for (int t = 0; t < TN; ++t) {
-                const float p0 = exp2_fast(z[t][0] - base), p1 = exp2_fast(z[t][1] - base);
-                l[n] += p0 + p1;
-                split2<X::HALF>(p0, p1, &pa[n][t / 2][(t & 1) * 2], &pa[n][t / 2][(t & 1) * 2 + 1]);
-            }
+                    for (int i = 0; i < 4; ++i) {
+                        const int hd = n * 8 + 2 * j + (i & 1);
+                        if (hd < heads) row[hd * A.score_len + t * 16 + (i >> 1) * 8] = s[n][t][i];
+                    }
         }
-        // o += p . v
+        if (__any_sync(FULL_MASK, grown)) {                   // rare after the first tiles of a row
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float top = m[n][e];
+#pragma unroll
+                    for (int t = 0; t < TN; ++t) top = fmaxf(top, fmaxf(s[n][t][e], s[n][t][e + 2]));
+                    top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 16));
+                    const float f = m[n][e] == -INFINITY ? 0.0f : exp2_fast(m[n][e] - top);
+                    m[n][e] = top;
+                    l[n][e] *= f;
+#pragma unroll
+                    for (int x = 0; x < KS; ++x) { o[n][x][e] *= f; o[n][x][e + 2] *= f; }
+                }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float base[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) base[e] = m[n][e] == -INFINITY ? 0.0f : m[n][e] - (X::HALF ? 15.0f : 0.0f);
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float p0 = exp2_fast(s[n][t][2 * i] - base[0]), p1 = exp2_fast(s[n][t][2 * i + 1] - base[1]);
+                    l[n][0] += p0;
+                    l[n][1] += p1;
+                    uint32_t hi, lo;
+                    split2<X::HALF>(p0, p1, &hi, &lo);
+                    ph[n][t][i] = transpose8x8(hi);
+                    pl[n][t][i] = transpose8x8(lo);
+                }
+        }
+        // o += v . p, elements x heads
+        const uint32_t sv = step();
+        if constexpr (RING & 1) load_values();
+        else load_keys();
+        auto vp = [&](int x, int t, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                mma16816<X::HALF>(o[n][x], a0, a1, a2, a3, ph[n][t][0], ph[n][t][1]);
+                mma16816<X::HALF>(o[n][x], a0, a1, a2, a3, pl[n][t][0], pl[n][t][1]);
+            }
+        };
         if constexpr (X::E8) {
 #pragma unroll
-            for (int kt = 0; kt < TN / 2; ++kt) {
-                const int r0 = kt * 16 + 2 * j;
+            for (int t = 0; t < TN; ++t) {
                 constexpr int W = X::DP / 32;                 // words of a lane's elements
-                uint32_t v[4][W];
+                uint32_t v[4][W];                             // tokens 2j, 2j+1, 2j+8, 2j+9
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int r = r0 + (i & 1) + (i >> 1) * 8;
+                    const int r = t * 16 + 2 * j + (i & 1) + (i >> 1) * 8;
                     if constexpr (X::CH == 4) {
                         const uint2 a = lds64(sv + place<X, true>(r, r8 >> 1) * 16 + (r8 & 1) * 8);
                         v[i][0] = a.x; v[i][1] = a.y;
@@ -721,77 +783,74 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
                     }
                 }
 #pragma unroll
-                for (int x = 0; x < VN; x += 2) {
-                    // bytes x, x+1 of two tokens each: (token 0, token 1) of element x, then of x+1
-                    const uint32_t sel = x & 2 ? 0x7362 : 0x5140;
-                    const uint32_t a = __byte_perm(v[0][x / 4], v[1][x / 4], sel), b = __byte_perm(v[2][x / 4], v[3][x / 4], sel);
-                    const uint32_t a0 = e4m3_to_f16(a), a1 = e4m3_to_f16(a >> 16), b0 = e4m3_to_f16(b), b1 = e4m3_to_f16(b >> 16);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        mma16816<true>(o[n][x], pa[n][kt][0], pa[n][kt][1], pa[n][kt][2], pa[n][kt][3], a0, b0);
-                        mma16816<true>(o[n][x + 1], pa[n][kt][0], pa[n][kt][1], pa[n][kt][2], pa[n][kt][3], a1, b1);
-                    }
+                for (int x = 0; x < KS; ++x) {
+                    // bytes 2x, 2x+1 of two tokens each: (token 0, token 1) of element 2x, then of 2x+1
+                    const uint32_t sel = x & 1 ? 0x7362 : 0x5140;
+                    const uint32_t a = __byte_perm(v[0][x / 2], v[1][x / 2], sel), b = __byte_perm(v[2][x / 2], v[3][x / 2], sel);
+                    vp(x, t, e4m3_to_f16(a), e4m3_to_f16(a >> 16), e4m3_to_f16(b), e4m3_to_f16(b >> 16));
                 }
             }
         } else {
 #pragma unroll
-            for (int kt = 0; kt < TN / 2; ++kt)
+            for (int x4 = 0; x4 < KS; x4 += 4) {
+                if (x4 * 16 >= A.c.dim) break;
 #pragma unroll
-                for (int x = 0; x < VN; x += 2) {
-                    if (x * 8 >= A.c.dim) break;
-                    uint32_t b[4];          // tokens 0-7 and 8-15, elements 0-7 of the tile x and of x+1
-                    ldmatrix4_trans(b, sv + place<X, true>(kt * 16 + (lane & 15), x + (lane >> 4)) * 16);
+                for (int x = 0; x < 4; ++x) {
+                    const uint32_t base = sv + vr * X::ROW + (((2 * x + vc) ^ vr) & 7) * 16;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        mma16816<X::HALF>(o[n][x], pa[n][kt][0], pa[n][kt][1], pa[n][kt][2], pa[n][kt][3], b[0], b[1]);
-                        mma16816<X::HALF>(o[n][x + 1], pa[n][kt][0], pa[n][kt][1], pa[n][kt][2], pa[n][kt][3], b[2], b[3]);
+                    for (int t = 0; t < TN; ++t) {
+                        uint32_t a[4];          // elements 0-7 and 8-15 of tokens 0-7, then of 8-15
+                        ldmatrix4_trans(a, base + t * 16 * X::ROW + x4 * 32);
+                        vp(x4 + x, t, a[0], a[1], a[2], a[3]);
                     }
                 }
+            }
         }
-#pragma unroll
-        for (int i = 0; i < X::STAGES - 1; ++i) there[i] = there[i + 1];
         // the row ends, or the span
         const bool row_ends = cc.tile + 1 == cc.end;
         if (row_ends || left == 1) {
             const int32_t g = cc.u / A.head_tiles, h0 = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS;
             const bool whole = begun_here && row_ends;
+            const float off = X::HALF ? 15.0f : 0.0f;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float sum = l[n];
-                sum += __shfl_xor_sync(FULL_MASK, sum, 1);
-                sum += __shfl_xor_sync(FULL_MASK, sum, 2);
-                const int hd = n * 8 + r8;
-                if (hd >= heads) continue;
-                const float off = X::HALF ? 15.0f : 0.0f;
-                if (whole) {
-                    const int64_t row = (int64_t)cc.b * A.q.heads + h0 + hd;
-                    Q* out = reinterpret_cast<Q*>(A.out.p + cc.b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
-                    const float f = sum == 0.0f ? 0.0f : A.c.v_scale / sum;
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int x = 0; x < VN; ++x)
+                for (int e = 0; e < 2; ++e) {
+                    float sum = l[n][e];
+                    sum += __shfl_xor_sync(FULL_MASK, sum, 4);
+                    sum += __shfl_xor_sync(FULL_MASK, sum, 8);
+                    sum += __shfl_xor_sync(FULL_MASK, sum, 16);
+                    const int hd = n * 8 + 2 * j + e;
+                    if (hd >= heads) continue;
+                    if (whole) {
+                        const int64_t row = (int64_t)cc.b * A.q.heads + h0 + hd;
+                        Q* out = reinterpret_cast<Q*>(A.out.p + cc.b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
+                        const float f = sum == 0.0f ? 0.0f : A.c.v_scale / sum;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int d = out_element<X>(x, j, e);
-                            if (d < A.c.dim) out[d] = from_float<Q>(sum == 0.0f ? 0.0f : both(o[n][x][e], o[n][x][e + 2]) * f);
+                        for (int x = 0; x < KS; ++x)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int d = out_element<X>(x, r8, i);
+                                if (d < A.c.dim) out[d] = from_float<Q>(sum == 0.0f ? 0.0f : o[n][x][i * 2 + e] * f);
+                            }
+                        if (r8 == 0) {
+                            const float y = sum == 0.0f ? -INFINITY : m[n][e] - off + log2f(sum);
+                            if (A.lse) A.lse[row] = y * 0.6931471805599453f;
+                            A.lse2[row] = y;
                         }
-                    if (j == 0) {
-                        const float y = sum == 0.0f ? -INFINITY : m[n] - off + log2f(sum);
-                        if (A.lse) A.lse[row] = y * 0.6931471805599453f;
-                        if (A.weight) A.lse2[row] = y;
+                    } else {
+                        float* part = A.part + ((int64_t)w * 2 + (first_piece ? 0 : 1)) * X::PART;
+                        if (r8 == 0) { part[hd] = m[n][e] - off; part[X::HEADS + hd] = sum; }
+                        part += 2 * X::HEADS + hd * X::DP;
+#pragma unroll
+                        for (int x = 0; x < KS; ++x)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int d = out_element<X>(x, r8, i);
+                                if (d < A.c.dim) part[d] = o[n][x][i * 2 + e];
+                            }
                     }
-                } else {
-                    float* part = A.part + ((int64_t)w * 2 + (first_piece ? 0 : 1)) * X::PART;
-                    if (j == 0) { part[hd] = m[n] - off; part[X::HEADS + hd] = sum; }
-                    part += 2 * X::HEADS + hd * X::DP;
-#pragma unroll
-                    for (int x = 0; x < VN; ++x)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int d = out_element<X>(x, j, e);
-                            if (d < A.c.dim) part[d] = both(o[n][x][e], o[n][x][e + 2]);
-                        }
                 }
-            }
             fresh = true;
             first_piece = false;
         }
@@ -799,16 +858,63 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
     }
 }
 
-// Rows that were cut into parts, and rows with nothing to attend to.  One row (sequence, query head) per `WPR` warps: few rows have
-// many parts each (WPR = 8: the warps share them), many rows few.
+// Elements of a row that came out as NaN although its scores are numbers, by one warp: an infinite value times the second half of a
+// probability, which may be 0 or negative, is no number, while the sum of p_t v_t is infinite.  They are summed with whole
+// probabilities, one token after the other.
+template <class X> __device__ __noinline__ void decode_repair(const DecodeArgs& A, int32_t b, int32_t h, float lse2) {
+    using Q = typename Elem<X::TQ>::T;
+    using C = typename Elem<X::TC>::T;
+    constexpr int PER = X::DP / 32;
+    const int lane = threadIdx.x & 31;
+    const int32_t g = h / A.group;
+    const Q* q = reinterpret_cast<const Q*>(A.q.p + b * A.q.sr + h * A.q.sh);
+    Q* out = reinterpret_cast<Q*>(A.out.p + b * A.out.sr + h * A.out.sh);
+    float o[PER];
+#pragma unroll
+    for (int x = 0; x < PER; ++x) o[x] = 0.0f;
+    int32_t lo, hi;
+    token_range(A, b, &lo, &hi);
+    for (int32_t t = lo; t < hi; ++t) {
+        const int32_t page = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
+        if ((unsigned)page >= (unsigned)A.c.n_pages) continue;
+        const int32_t at = t & ((1 << A.c.page_shift) - 1);
+        const C* k = reinterpret_cast<const C*>(A.c.k + page * A.c.ks[0] + at * A.c.ks[1] + g * A.c.ks[2]);
+        const C* v = reinterpret_cast<const C*>(A.c.v + page * A.c.vs[0] + at * A.c.vs[1] + g * A.c.vs[2]);
+        float s = 0.0f;
+        for (int d = lane; d < A.c.dim; d += 32) s += to_float(q[d]) * to_float(k[d]);
+        for (int w = 16; w; w >>= 1) s += __shfl_xor_sync(FULL_MASK, s, w);
+        s *= A.scale * A.c.k_scale * 1.4426950408889634f;
+        if (s == -INFINITY) continue;
+        const float p = exp2f(s - lse2);
+#pragma unroll
+        for (int x = 0; x < PER; ++x)
+            if (lane + 32 * x < A.c.dim) o[x] += p * to_float(v[lane + 32 * x]);
+    }
+#pragma unroll
+    for (int x = 0; x < PER; ++x)
+        if (lane + 32 * x < A.c.dim && to_float(out[lane + 32 * x]) != to_float(out[lane + 32 * x])) out[lane + 32 * x] = from_float<Q>(o[x] * A.c.v_scale);
+}
+template <class X> __device__ __forceinline__ void decode_check(const DecodeArgs& A, int32_t b, int32_t h, float lse2) {
+    using Q = typename Elem<X::TQ>::T;
+    const Q* out = reinterpret_cast<const Q*>(A.out.p + b * A.out.sr + h * A.out.sh);
+    bool bad = false;
+    for (int d = threadIdx.x & 31; d < A.c.dim; d += 32) bad |= to_float(out[d]) != to_float(out[d]);
+    if (__any_sync(FULL_MASK, bad) && lse2 == lse2) decode_repair<X>(A, b, h, lse2);
+}
+
+// Rows that were cut into parts, and rows with nothing to attend to.  WPR = 8: a CTA per row (sequence, query head), where few rows have
+// many parts each: first the factor of every part from its m, then the parts' outputs by eight warps.  WPR = 1: a warp per row, where many
+// rows have few.
 template <class X, int WPR>
-__global__ void __launch_bounds__(256) decode_join_kernel(const DecodeArgs A) {
+__global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant__ DecodeArgs A) {
     using Q = typename Elem<X::TQ>::T;
     constexpr int PER = X::DP / 32;
-    __shared__ float s_m[8], s_l[8], s_o[WPR == 1 ? 1 : 8][X::DP];
+    constexpr int MOST = WPR == 8 ? KLPM_SMS * 4 * KLPM_DECODE_WARPS : 1;
+    __shared__ float s_f[MOST];                              // m of the parts, then their factors
+    __shared__ float s_red[8], s_o[WPR == 8 ? 8 : 1][X::DP];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row = WPR == 8 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + warp;
     if (row >= (int64_t)A.n_seqs * A.q.heads) return;
     const int32_t b = (int32_t)(row / A.q.heads), h = (int32_t)(row % A.q.heads), g = h / A.group, i = h - g * A.group;
@@ -816,64 +922,80 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const DecodeArgs A) {
     const long long t0 = A.tiles_before[b], tiles = A.tiles_before[b + 1] - t0;
     const long long span = span_of(A.tiles_before[A.n_seqs] * A.units, A.warps);
     const long long R = t0 * A.units + u * tiles, E = R + tiles;
-    const long long w0 = R / span, w1 = (E - 1) / span;
-    if (tiles > 0 && w0 == w1) return;                       // decode_kernel has written it
-    const int part_of = WPR == 8 ? warp : 0;
+    const int32_t w0 = (int32_t)(R / span), parts = tiles > 0 ? (int32_t)((E - 1) / span) - w0 + 1 : 0;
+    if (parts == 1) {                                        // decode_kernel has written it
+        if (WPR == 1 || warp == 0) decode_check<X>(A, b, h, A.lse2[row]);
+        return;
+    }
+    const int first = w0 * span == R ? 0 : 1;
+    auto part = [&](int k) -> const float* { return A.part + ((int64_t)(w0 + k) * 2 + (k == 0 ? first : 0)) * X::PART; };
     float m = -INFINITY, l = 0.0f, o[PER];
 #pragma unroll
-    for (int k = 0; k < PER; ++k) o[k] = 0.0f;
-    if (tiles > 0) {
-        const long long first = w0 * span == R ? w0 * 2 : w0 * 2 + 1;
-        for (long long w = w0 + part_of; w <= w1; w += WPR) {
-            const float* p = A.part + (w == w0 ? first : w * 2) * X::PART;
-            const float pm = p[hd], pl = p[X::HEADS + hd];
-            float v[PER];
+    for (int x = 0; x < PER; ++x) o[x] = 0.0f;
+    if constexpr (WPR == 8) {
+        for (int k = tid; k < parts; k += 256) { s_f[k] = part(k)[hd]; m = fmaxf(m, s_f[k]); }
+        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL_MASK, m, d));
+        if (lane == 0) s_red[warp] = m;
+        __syncthreads();
+        for (int k = 0; k < 8; ++k) m = fmaxf(m, s_red[k]);
+        const float base = m == -INFINITY ? 0.0f : m;
+        __syncthreads();
+        for (int k = tid; k < parts; k += 256) {
+            const float f = exp2_fast(s_f[k] - base);
+            l += f * part(k)[X::HEADS + hd];
+            s_f[k] = f;
+        }
+        for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(FULL_MASK, l, d);
+        if (lane == 0) s_red[warp] = l;
+        __syncthreads();
+        l = 0.0f;
+        for (int k = 0; k < 8; ++k) l += s_red[k];
+#pragma unroll 4
+        for (int k = warp; k < parts; k += 8) {
+            const float* p = part(k) + 2 * X::HEADS + hd * X::DP + lane;
+            const float f = s_f[k];
 #pragma unroll
-            for (int k = 0; k < PER; ++k) v[k] = lane + 32 * k < A.c.dim ? p[2 * X::HEADS + hd * X::DP + lane + 32 * k] : 0.0f;
+            for (int x = 0; x < PER; ++x)
+                if (lane + 32 * x < A.c.dim) o[x] += f * p[32 * x];
+        }
+#pragma unroll
+        for (int x = 0; x < PER; ++x) s_o[warp][lane + 32 * x] = o[x];
+        __syncthreads();
+        if (warp) return;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+            o[x] = 0.0f;
+            for (int k = 0; k < 8; ++k) o[x] += s_o[k][lane + 32 * x];
+        }
+    } else {
+        for (int k = 0; k < parts; ++k) {
+            const float* p = part(k);
+            const float pm = p[hd], pl = p[X::HEADS + hd];
             const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.0f : top;
             const float f = exp2_fast(m - base), pf = exp2_fast(pm - base);
             m = top;
             l = l * f + pl * pf;
 #pragma unroll
-            for (int k = 0; k < PER; ++k) o[k] = o[k] * f + v[k] * pf;
+            for (int x = 0; x < PER; ++x) o[x] = o[x] * f + (lane + 32 * x < A.c.dim ? p[2 * X::HEADS + hd * X::DP + lane + 32 * x] : 0.0f) * pf;
         }
-    }
-    if constexpr (WPR == 8) {
-        if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
-#pragma unroll
-        for (int k = 0; k < PER; ++k) s_o[warp][lane + 32 * k] = o[k];
-        __syncthreads();
-        if (warp) return;
-        float top = -INFINITY;
-        for (int w = 0; w < 8; ++w) top = fmaxf(top, s_m[w]);
-        const float base = top == -INFINITY ? 0.0f : top;
-        l = 0.0f;
-#pragma unroll
-        for (int k = 0; k < PER; ++k) o[k] = 0.0f;
-        for (int w = 0; w < 8; ++w) {
-            const float f = exp2_fast(s_m[w] - base);
-            l += s_l[w] * f;
-#pragma unroll
-            for (int k = 0; k < PER; ++k) o[k] += s_o[w][lane + 32 * k] * f;
-        }
-        m = top;
     }
     Q* out = reinterpret_cast<Q*>(A.out.p + b * A.out.sr + h * A.out.sh);
     const float f = l == 0.0f ? 0.0f : A.c.v_scale / l;
 #pragma unroll
-    for (int k = 0; k < PER; ++k)
-        if (lane + 32 * k < A.c.dim) out[lane + 32 * k] = from_float<Q>(l == 0.0f ? 0.0f : o[k] * f);
+    for (int x = 0; x < PER; ++x)
+        if (lane + 32 * x < A.c.dim) out[lane + 32 * x] = from_float<Q>(l == 0.0f ? 0.0f : o[x] * f);
+    const float y = l == 0.0f ? -INFINITY : m + log2f(l);
     if (lane == 0) {
-        const float y = l == 0.0f ? -INFINITY : m + log2f(l);
         if (A.lse) A.lse[row] = y * 0.6931471805599453f;
-        if (A.weight) A.lse2[row] = y;
+        A.lse2[row] = y;
     }
+    decode_check<X>(A, b, h, y);
 }
 
 // What every token received, from the scores that decode_kernel kept: a warp takes a span of tiles of the batch, in the order (sequence,
 // cache head, tile).  One thread adds up a token's heads, so that the order of the sum is fixed.
 template <int TT>
-__global__ void __launch_bounds__(256) decode_weight_kernel(const DecodeArgs A) {
+__global__ void __launch_bounds__(256) decode_weight_kernel(const __grid_constant__ DecodeArgs A) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const int32_t w = blockIdx.x * 8 + (threadIdx.x >> 5), warps = gridDim.x * 8;
@@ -919,7 +1041,7 @@ struct DecodeSpace { int64_t lse2, part, score, score_len, bytes; };
 DecodeSpace decode_space(int64_t n_seqs, int64_t heads, int64_t max_tokens, int64_t warps, int64_t part, bool weight) {
     DecodeSpace s;
     s.lse2 = up256((n_seqs + 1) * 8);
-    s.part = s.lse2 + (weight ? up256(n_seqs * heads * 4) : 0);
+    s.part = s.lse2 + up256(n_seqs * heads * 4);
     s.score = s.part + up256(warps * 2 * part * 4);
     s.score_len = (max_tokens + 31) / 32 * 32;
     s.bytes = s.score + (weight ? up256(n_seqs * heads * s.score_len * 4) : 0);
