@@ -8,6 +8,7 @@
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <atomic>
 
 #include "klpm_kv.h"
 
@@ -298,6 +299,8 @@ struct DecodeArgs {
 #define KLPM_DECODE_WARPS 4             // of a CTA
 #define KLPM_DECODE_MIN_SPAN 2          // tiles
 #define KLPM_SMS 148
+#define KLPM_ROW_TOKENS 16384            // the most a sequence may have, and tiles per warp of the GPU, for decode_row_kernel
+#define KLPM_ROW_TILES 8
 
 template <int TQ_, int TC_, int DP_, int NT_> struct Dec {
     static constexpr int TQ = TQ_, TC = TC_, DP = DP_, NT = NT_;
@@ -438,77 +441,16 @@ template <class X> struct Cursor {       // a tile of the batch
     }
 };
 
-template <class X>
-__global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel(const __grid_constant__ DecodeArgs A) {
+// One warp computes `left` tiles of the batch from ci on.  finish(tile, begun, ended, heads, m, l, o) is called with what a row came to when the
+// row or the span ends: begun and ended say whether the warp had the row's first and last tile.
+template <class X, class F>
+__device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, unsigned* s_there, Cursor<X> ci, long long left, F finish) {
     using Q = typename Elem<X::TQ>::T;
     constexpr int TT = X::TT, KS = X::DP / 16, TN = TT / 16, NT = X::NT, RING = X::RING;
-    extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ long long s_sum[KLPM_DECODE_WARPS];
-    __shared__ int32_t s_b[KLPM_DECODE_WARPS];
-    __shared__ long long s_rem[KLPM_DECODE_WARPS];
-    __shared__ unsigned s_there[KLPM_DECODE_WARPS][8];         // which tokens of the tiles on their way are there
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31;
     const int32_t chunks = A.c.dim * (X::E8 ? 1 : 2) / 16;
-    if (chunks < X::CH)                                       // elements behind dim stay 0
-        for (int i = tid; i < X::SMEM / 16; i += KLPM_DECODE_WARPS * 32) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
-    // where each warp starts: every CTA adds up the tiles of all sequences
-    const int32_t per = (A.n_seqs + KLPM_DECODE_WARPS * 32 - 1) / (KLPM_DECODE_WARPS * 32);
-    const int32_t b0 = min(tid * per, A.n_seqs), b1 = min(b0 + per, A.n_seqs);
-    long long mine = 0;
-    int32_t first;
-    for (int32_t b = b0; b < b1; ++b) mine += tiles_of<TT>(A, b, &first);
-    long long before = mine;
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long v = __shfl_up_sync(FULL_MASK, before, d);
-        if (lane >= d) before += v;
-    }
-    if (lane == 31) s_sum[warp] = before;
-    before -= mine;
-    __syncthreads();
-    long long total = 0;
-    for (int w = 0; w < KLPM_DECODE_WARPS; ++w) {
-        if (w < warp) before += s_sum[w];
-        total += s_sum[w];
-    }
-    if (blockIdx.x == 0) {
-        long long at = before;
-        for (int32_t b = b0; b < b1; ++b) { A.tiles_before[b] = at; at += tiles_of<TT>(A, b, &first); }
-        if (tid == 0) A.tiles_before[A.n_seqs] = total;
-    }
-    total *= A.units;
-    const long long span = span_of(total, A.warps);
-    for (int w = 0; w < KLPM_DECODE_WARPS; ++w) {
-        const long long pos = ((long long)w * gridDim.x + blockIdx.x) * span;
-        if (pos < total && pos >= before * A.units && pos < (before + mine) * A.units) {
-            long long rem = pos - before * A.units;
-            int32_t b = b0;
-            for (;; ++b) {
-                const long long n = (long long)tiles_of<TT>(A, b, &first) * A.units;
-                if (rem < n) break;
-                rem -= n;
-            }
-            s_b[w] = b; s_rem[w] = rem;
-        }
-    }
-    __syncthreads();
-    const int32_t w = warp * gridDim.x + blockIdx.x;          // neighbouring spans on different SMs
-    const long long pos = (long long)w * span;
-    if (pos >= total) return;
-    long long left = min(span, total - pos);                  // tiles to compute
-
-    Cursor<X> ci;                                             // the tile that is loaded next
-    ci.b = s_b[warp]; ci.u = 0;
-    ci.row(A);
-    {
-        const long long rem = s_rem[warp];
-        ci.u = (int32_t)(rem / (ci.end - ci.first));
-        ci.tile = ci.first + (int32_t)(rem % (ci.end - ci.first));
-    }
-    Cursor<X> cc = ci;                                        // the tile that is computed next
+    Cursor<X> cc = ci;                                        // the tile that is computed next (ci: the one that is loaded next)
     long long to_load = left;
-
-    const uint32_t ring = smem_addr(smem) + warp * X::WARP_SMEM;
     const int32_t in_page = (1 << A.c.page_shift) - 1;
     const int my_row = lane / X::CH % TT, my_ch = lane % X::CH;
     // the page of token `lane` of the tile at ci; -1: nothing there
@@ -553,7 +495,7 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
             at = (ci.tile * TT + lane) & in_page;
             g_now = ci.u / A.head_tiles;
             const unsigned there = __ballot_sync(FULL_MASK, page >= 0);
-            if (lane == 0) s_there[warp][tile_in & 7] = there;
+            if (lane == 0) s_there[tile_in & 7] = there;
             ++tile_in;
             if (to_load > 1) {
                 ci.next(A);
@@ -578,7 +520,7 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
     const int kr = lane & 15, kc = lane >> 4, vr = (lane & 7) + ((lane >> 4) << 3), vc = (lane >> 3) & 1;
     uint32_t qb[X::QF][NT][KS][2];
     float coef[NT][2], m[NT][2], l[NT][2], o[NT][KS][4];
-    bool fresh = true, begun_here = false, first_piece = true;
+    bool fresh = true, begun_here = false;
     int32_t heads = 0;
     int slot_out = 0, tile_out = 0;
     auto step = [&]() -> uint32_t {                           // the next half tile has arrived, and the one before it is no longer read
@@ -689,7 +631,7 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
             }
         }
         // p = 2^(s - m): tokens r8 and r8 + 8 of heads 2j and 2j + 1
-        const unsigned have = s_there[warp][tile_out++ & 7];
+        const unsigned have = s_there[tile_out++ & 7];
         uint32_t ph[NT][TN][2], pl[NT][TN][2];
         bool grown = false;
 #pragma unroll
@@ -809,53 +751,148 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
         // the row ends, or the span
         const bool row_ends = cc.tile + 1 == cc.end;
         if (row_ends || left == 1) {
-            const int32_t g = cc.u / A.head_tiles, h0 = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS;
-            const bool whole = begun_here && row_ends;
-            const float off = X::HALF ? 15.0f : 0.0f;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float sum = l[n][e];
-                    sum += __shfl_xor_sync(FULL_MASK, sum, 4);
-                    sum += __shfl_xor_sync(FULL_MASK, sum, 8);
-                    sum += __shfl_xor_sync(FULL_MASK, sum, 16);
-                    const int hd = n * 8 + 2 * j + e;
-                    if (hd >= heads) continue;
-                    if (whole) {
-                        const int64_t row = (int64_t)cc.b * A.q.heads + h0 + hd;
-                        Q* out = reinterpret_cast<Q*>(A.out.p + cc.b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
-                        const float f = sum == 0.0f ? 0.0f : A.c.v_scale / sum;
-#pragma unroll
-                        for (int x = 0; x < KS; ++x)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const int d = out_element<X>(x, r8, i);
-                                if (d < A.c.dim) out[d] = from_float<Q>(sum == 0.0f ? 0.0f : o[n][x][i * 2 + e] * f);
-                            }
-                        if (r8 == 0) {
-                            const float y = sum == 0.0f ? -INFINITY : m[n][e] - off + log2f(sum);
-                            if (A.lse) A.lse[row] = y * 0.6931471805599453f;
-                            A.lse2[row] = y;
-                        }
-                    } else {
-                        float* part = A.part + ((int64_t)w * 2 + (first_piece ? 0 : 1)) * X::PART;
-                        if (r8 == 0) { part[hd] = m[n][e] - off; part[X::HEADS + hd] = sum; }
-                        part += 2 * X::HEADS + hd * X::DP;
-#pragma unroll
-                        for (int x = 0; x < KS; ++x)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const int d = out_element<X>(x, r8, i);
-                                if (d < A.c.dim) part[d] = o[n][x][i * 2 + e];
-                            }
-                    }
+                    l[n][e] += __shfl_xor_sync(FULL_MASK, l[n][e], 4);
+                    l[n][e] += __shfl_xor_sync(FULL_MASK, l[n][e], 8);
+                    l[n][e] += __shfl_xor_sync(FULL_MASK, l[n][e], 16);
+                    m[n][e] -= X::HALF ? 15.0f : 0.0f;
                 }
+            finish(cc, begun_here, row_ends, heads, m, l, o);
             fresh = true;
-            first_piece = false;
         }
         if (left > 1) cc.next(A);
     }
+}
+
+// Elements behind dim are 0 in shared memory throughout.
+template <class X> __device__ __forceinline__ void clear_ring(const DecodeArgs& A, unsigned char* smem, int bytes) {
+    if (A.c.dim * (X::E8 ? 1 : 2) / 16 < X::CH)
+        for (int i = threadIdx.x; i < bytes / 16; i += blockDim.x) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+}
+// A row's result, where a warp has all of it.
+template <class X> __device__ __forceinline__ void write_part(float* part, int32_t heads, const float (&m)[X::NT][2], const float (&l)[X::NT][2],
+                                                              const float (&o)[X::NT][X::DP / 16][4], int32_t dim) {
+    const int lane = threadIdx.x & 31, r8 = lane >> 2, j = lane & 3;
+#pragma unroll
+    for (int n = 0; n < X::NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int hd = n * 8 + 2 * j + e;
+            if (hd >= heads) continue;
+            if (r8 == 0) { part[hd] = m[n][e]; part[X::HEADS + hd] = l[n][e]; }
+            float* y = part + 2 * X::HEADS + hd * X::DP;
+#pragma unroll
+            for (int x = 0; x < X::DP / 16; ++x)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int d = out_element<X>(x, r8, i);
+                    if (d < dim) y[d] = o[n][x][i * 2 + e];
+                }
+        }
+}
+
+
+template <class X>
+__global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel(const __grid_constant__ DecodeArgs A) {
+    using Q = typename Elem<X::TQ>::T;
+    constexpr int TT = X::TT, KS = X::DP / 16, NT = X::NT;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ long long s_sum[KLPM_DECODE_WARPS];
+    __shared__ int32_t s_b[KLPM_DECODE_WARPS];
+    __shared__ long long s_rem[KLPM_DECODE_WARPS];
+    __shared__ unsigned s_there[KLPM_DECODE_WARPS][8];         // which tokens of the tiles on their way are there
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    clear_ring<X>(A, smem, X::SMEM);
+    // where each warp starts: every CTA adds up the tiles of all sequences
+    const int32_t per = (A.n_seqs + KLPM_DECODE_WARPS * 32 - 1) / (KLPM_DECODE_WARPS * 32);
+    const int32_t b0 = min(tid * per, A.n_seqs), b1 = min(b0 + per, A.n_seqs);
+    long long mine = 0;
+    int32_t first;
+    for (int32_t b = b0; b < b1; ++b) mine += tiles_of<TT>(A, b, &first);
+    long long before = mine;
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long v = __shfl_up_sync(FULL_MASK, before, d);
+        if (lane >= d) before += v;
+    }
+    if (lane == 31) s_sum[warp] = before;
+    before -= mine;
+    __syncthreads();
+    long long total = 0;
+    for (int w = 0; w < KLPM_DECODE_WARPS; ++w) {
+        if (w < warp) before += s_sum[w];
+        total += s_sum[w];
+    }
+    if (blockIdx.x == 0) {
+        long long at = before;
+        for (int32_t b = b0; b < b1; ++b) { A.tiles_before[b] = at; at += tiles_of<TT>(A, b, &first); }
+        if (tid == 0) A.tiles_before[A.n_seqs] = total;
+    }
+    total *= A.units;
+    const long long span = span_of(total, A.warps);
+    for (int w = 0; w < KLPM_DECODE_WARPS; ++w) {
+        const long long pos = ((long long)w * gridDim.x + blockIdx.x) * span;
+        if (pos < total && pos >= before * A.units && pos < (before + mine) * A.units) {
+            long long rem = pos - before * A.units;
+            int32_t b = b0;
+            for (;; ++b) {
+                const long long n = (long long)tiles_of<TT>(A, b, &first) * A.units;
+                if (rem < n) break;
+                rem -= n;
+            }
+            s_b[w] = b; s_rem[w] = rem;
+        }
+    }
+    __syncthreads();
+    const int32_t w = warp * gridDim.x + blockIdx.x;          // neighbouring spans on different SMs
+    const long long pos = (long long)w * span;
+    if (pos >= total) return;
+
+    Cursor<X> ci;                                             // the tile that is loaded next
+    ci.b = s_b[warp]; ci.u = 0;
+    ci.row(A);
+    {
+        const long long rem = s_rem[warp];
+        ci.u = (int32_t)(rem / (ci.end - ci.first));
+        ci.tile = ci.first + (int32_t)(rem % (ci.end - ci.first));
+    }
+    bool first_piece = true;
+    decode_span<X>(A, smem_addr(smem) + warp * X::WARP_SMEM, s_there[warp], ci, min(span, total - pos),
+                   [&](const Cursor<X>& cc, bool begun, bool ended, int32_t heads, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[NT][KS][4]) {
+        if (!begun || !ended) {
+            write_part<X>(A.part + ((int64_t)w * 2 + (first_piece ? 0 : 1)) * X::PART, heads, m, l, o, A.c.dim);
+        } else {
+            const int r8 = lane >> 2, j = lane & 3;
+            const int32_t g = cc.u / A.head_tiles, h0 = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int hd = n * 8 + 2 * j + e;
+                    if (hd >= heads) continue;
+                    const float sum = l[n][e];
+                    Q* out = reinterpret_cast<Q*>(A.out.p + cc.b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
+                    const float f = sum == 0.0f ? 0.0f : A.c.v_scale / sum;
+#pragma unroll
+                    for (int x = 0; x < KS; ++x)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int d = out_element<X>(x, r8, i);
+                            if (d < A.c.dim) out[d] = from_float<Q>(sum == 0.0f ? 0.0f : o[n][x][i * 2 + e] * f);
+                        }
+                    if (r8 == 0) {
+                        const int64_t row = (int64_t)cc.b * A.q.heads + h0 + hd;
+                        const float y = sum == 0.0f ? -INFINITY : m[n][e] + log2f(sum);
+                        if (A.lse) A.lse[row] = y * 0.6931471805599453f;
+                        A.lse2[row] = y;
+                    }
+                }
+        }
+        first_piece = false;
+    });
 }
 
 // Elements of a row that came out as NaN although its scores are numbers, by one warp: an infinite value times the second half of a
@@ -903,18 +940,15 @@ template <class X> __device__ __forceinline__ void decode_check(const DecodeArgs
 }
 
 // Rows that were cut into parts, and rows with nothing to attend to.  WPR = 8: a CTA per row (sequence, query head), where few rows have
-// many parts each: first the factor of every part from its m, then the parts' outputs by eight warps.  WPR = 1: a warp per row, where many
-// rows have few.
+// many parts each.  WPR = 1: a warp per row, where many rows have few.
 template <class X, int WPR>
 __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant__ DecodeArgs A) {
     using Q = typename Elem<X::TQ>::T;
     constexpr int PER = X::DP / 32;
-    constexpr int MOST = WPR == 8 ? KLPM_SMS * 4 * KLPM_DECODE_WARPS : 1;
-    __shared__ float s_f[MOST];                              // m of the parts, then their factors
-    __shared__ float s_red[8], s_o[WPR == 8 ? 8 : 1][X::DP];
+    __shared__ float s_m[8], s_l[8], s_o[WPR == 8 ? 8 : 1][X::DP];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = WPR == 8 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + warp;
     if (row >= (int64_t)A.n_seqs * A.q.heads) return;
     const int32_t b = (int32_t)(row / A.q.heads), h = (int32_t)(row % A.q.heads), g = h / A.group, i = h - g * A.group;
@@ -932,64 +966,176 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
     float m = -INFINITY, l = 0.0f, o[PER];
 #pragma unroll
     for (int x = 0; x < PER; ++x) o[x] = 0.0f;
-    if constexpr (WPR == 8) {
-        for (int k = tid; k < parts; k += 256) { s_f[k] = part(k)[hd]; m = fmaxf(m, s_f[k]); }
-        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL_MASK, m, d));
-        if (lane == 0) s_red[warp] = m;
-        __syncthreads();
-        for (int k = 0; k < 8; ++k) m = fmaxf(m, s_red[k]);
-        const float base = m == -INFINITY ? 0.0f : m;
-        __syncthreads();
-        for (int k = tid; k < parts; k += 256) {
-            const float f = exp2_fast(s_f[k] - base);
-            l += f * part(k)[X::HEADS + hd];
-            s_f[k] = f;
-        }
-        for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(FULL_MASK, l, d);
-        if (lane == 0) s_red[warp] = l;
-        __syncthreads();
-        l = 0.0f;
-        for (int k = 0; k < 8; ++k) l += s_red[k];
-#pragma unroll 4
-        for (int k = warp; k < parts; k += 8) {
-            const float* p = part(k) + 2 * X::HEADS + hd * X::DP + lane;
-            const float f = s_f[k];
+    constexpr int DEEP = 4;                                  // parts of a warp whose loads are in flight together
+    for (int32_t k0 = WPR == 8 ? warp : 0; k0 < parts; k0 += WPR * DEEP) {
+        float pm[DEEP], pl[DEEP], v[DEEP][PER];
 #pragma unroll
-            for (int x = 0; x < PER; ++x)
-                if (lane + 32 * x < A.c.dim) o[x] += f * p[32 * x];
+        for (int y = 0; y < DEEP; ++y) {
+            const bool some = k0 + y * WPR < parts;
+            const float* p = part(some ? k0 + y * WPR : k0);
+            pm[y] = some ? p[hd] : -INFINITY;
+            pl[y] = some ? p[X::HEADS + hd] : 0.0f;
+#pragma unroll
+            for (int x = 0; x < PER; ++x) v[y][x] = some && lane + 32 * x < A.c.dim ? p[2 * X::HEADS + hd * X::DP + lane + 32 * x] : 0.0f;
         }
+        float top = m;
+#pragma unroll
+        for (int y = 0; y < DEEP; ++y) top = fmaxf(top, pm[y]);
+        const float base = top == -INFINITY ? 0.0f : top, f = exp2_fast(m - base);
+        m = top;
+        l *= f;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) o[x] *= f;
+#pragma unroll
+        for (int y = 0; y < DEEP; ++y) {
+            const float pf = exp2_fast(pm[y] - base);
+            l += pl[y] * pf;
+#pragma unroll
+            for (int x = 0; x < PER; ++x) o[x] += v[y][x] * pf;
+        }
+    }
+    if constexpr (WPR == 8) {
+        if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
 #pragma unroll
         for (int x = 0; x < PER; ++x) s_o[warp][lane + 32 * x] = o[x];
         __syncthreads();
         if (warp) return;
+        for (int k = 0; k < 8; ++k) m = fmaxf(m, s_m[k]);
+        const float base = m == -INFINITY ? 0.0f : m;
+        l = 0.0f;
 #pragma unroll
-        for (int x = 0; x < PER; ++x) {
-            o[x] = 0.0f;
-            for (int k = 0; k < 8; ++k) o[x] += s_o[k][lane + 32 * x];
-        }
-    } else {
-        for (int k = 0; k < parts; ++k) {
-            const float* p = part(k);
-            const float pm = p[hd], pl = p[X::HEADS + hd];
-            const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.0f : top;
-            const float f = exp2_fast(m - base), pf = exp2_fast(pm - base);
-            m = top;
-            l = l * f + pl * pf;
+        for (int x = 0; x < PER; ++x) o[x] = 0.0f;
+        for (int k = 0; k < 8; ++k) {
+            const float f = exp2_fast(s_m[k] - base);
+            l += s_l[k] * f;
 #pragma unroll
-            for (int x = 0; x < PER; ++x) o[x] = o[x] * f + (lane + 32 * x < A.c.dim ? p[2 * X::HEADS + hd * X::DP + lane + 32 * x] : 0.0f) * pf;
+            for (int x = 0; x < PER; ++x) o[x] += s_o[k][lane + 32 * x] * f;
         }
     }
     Q* out = reinterpret_cast<Q*>(A.out.p + b * A.out.sr + h * A.out.sh);
     const float f = l == 0.0f ? 0.0f : A.c.v_scale / l;
+    bool bad = false;
 #pragma unroll
     for (int x = 0; x < PER; ++x)
-        if (lane + 32 * x < A.c.dim) out[lane + 32 * x] = from_float<Q>(l == 0.0f ? 0.0f : o[x] * f);
+        if (lane + 32 * x < A.c.dim) {
+            const float z = l == 0.0f ? 0.0f : o[x] * f;
+            out[lane + 32 * x] = from_float<Q>(z);
+            bad |= z != z;
+        }
     const float y = l == 0.0f ? -INFINITY : m + log2f(l);
     if (lane == 0) {
         if (A.lse) A.lse[row] = y * 0.6931471805599453f;
         A.lse2[row] = y;
     }
-    decode_check<X>(A, b, h, y);
+    if (__any_sync(FULL_MASK, bad) && y == y) decode_repair<X>(A, b, h, y);
+}
+
+// Small calls: a cluster of CTAs per row (sequence, unit), its tiles dealt out to all of the cluster's warps, whose results are joined through
+// distributed shared memory: one kernel, no trip through the workspace.  Weights are added from the scores by the warps that made them.
+#define KLPM_ROW_WARPS 8
+template <class X>
+__global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_kernel(const __grid_constant__ DecodeArgs A, int32_t ctas) {
+    using Q = typename Elem<X::TQ>::T;
+    constexpr int TT = X::TT, KS = X::DP / 16, NT = X::NT, MOST = 8 * KLPM_ROW_WARPS;
+    static_assert(X::PART * 4 <= X::WARP_SMEM, "a warp's result lies in its ring");
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ unsigned s_there[KLPM_ROW_WARPS][8];
+    __shared__ float s_f[X::HEADS][MOST], s_lse2[X::HEADS], s_scale[X::HEADS], s_o[KLPM_ROW_WARPS * 32];
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int32_t rank = blockIdx.x % ctas, row = blockIdx.x / ctas;
+    Cursor<X> c;
+    c.b = row / A.units; c.u = row - c.b * A.units;
+    token_range(A, c.b, &c.lo, &c.hi);
+    c.first = c.lo / TT;
+    c.end = c.hi > c.lo ? (c.hi + TT - 1) / TT : c.first;
+    const int32_t tiles = c.end - c.first, warps = ctas * KLPM_ROW_WARPS, per = (tiles + warps - 1) / warps;
+    const int32_t parts = per > 0 ? (tiles + per - 1) / per : 0;
+    const int32_t g = c.u / A.head_tiles, h0 = g * A.group + (c.u - g * A.head_tiles) * X::HEADS;
+    const int32_t heads = min(X::HEADS, A.group - (c.u - g * A.head_tiles) * X::HEADS);
+    clear_ring<X>(A, smem, KLPM_ROW_WARPS * X::WARP_SMEM);
+    __syncthreads();
+    const int32_t mine = warp * ctas + rank;                  // neighbouring parts on different SMs
+    float* part = reinterpret_cast<float*>(smem + warp * X::WARP_SMEM);
+    const int32_t from = c.first + mine * per, count = min(per, c.end - from);
+    if (mine < parts) {
+        c.tile = from;
+        decode_span<X>(A, smem_addr(smem) + warp * X::WARP_SMEM, s_there[warp], c, count,
+                       [&](const Cursor<X>&, bool, bool, int32_t, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[NT][KS][4]) {
+            cp_async_wait<0>();
+            __syncwarp();
+            write_part<X>(part, heads, m, l, o, A.c.dim);
+        });
+    }
+    cluster.sync();
+    // the factor of every part, and the sum, of every head
+    for (int hd = warp; hd < heads; hd += KLPM_ROW_WARPS) {
+        float pm[MOST / 32], m = -INFINITY, l = 0.0f;
+#pragma unroll
+        for (int i = 0; i < MOST / 32; ++i) {
+            const int k = lane + 32 * i;
+            pm[i] = k < parts ? reinterpret_cast<const float*>(cluster.map_shared_rank(smem, k % ctas) + k / ctas * X::WARP_SMEM)[hd] : -INFINITY;
+            m = fmaxf(m, pm[i]);
+        }
+        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL_MASK, m, d));
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int i = 0; i < MOST / 32; ++i) {
+            const int k = lane + 32 * i;
+            if (k >= parts) continue;
+            const float f = exp2_fast(pm[i] - base);
+            l += f * reinterpret_cast<const float*>(cluster.map_shared_rank(smem, k % ctas) + k / ctas * X::WARP_SMEM)[X::HEADS + hd];
+            s_f[hd][k] = f;
+        }
+        for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(FULL_MASK, l, d);
+        if (lane == 0) {
+            s_lse2[hd] = l == 0.0f ? -INFINITY : m + log2f(l);
+            s_scale[hd] = l == 0.0f ? 0.0f : A.c.v_scale / l;
+        }
+    }
+    __syncthreads();
+    // outputs: a head per CTA at a time, an element per thread, the parts shared by the threads that are left
+    constexpr int SLICES = KLPM_ROW_WARPS * 32 / X::DP;
+    const int d = tid % X::DP, slice = tid / X::DP;
+    for (int hd = rank; hd < heads; hd += ctas) {
+        float y = 0.0f;
+        if (d < A.c.dim) {
+#pragma unroll 4
+            for (int k = slice; k < parts; k += SLICES)
+                y += s_f[hd][k] * reinterpret_cast<const float*>(cluster.map_shared_rank(smem, k % ctas) + k / ctas * X::WARP_SMEM)[2 * X::HEADS + hd * X::DP + d];
+        }
+        if (SLICES > 1) {
+            __syncthreads();
+            s_o[tid] = y;
+            __syncthreads();
+            if (slice == 0)
+                for (int i = 1; i < SLICES; ++i) y += s_o[i * X::DP + d];
+        }
+        const float lse2 = s_lse2[hd];
+        bool bad = false;
+        if (slice == 0 && d < A.c.dim) {
+            y = lse2 == -INFINITY ? 0.0f : y * s_scale[hd];
+            reinterpret_cast<Q*>(A.out.p + c.b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh)[d] = from_float<Q>(y);
+            bad = y != y;
+        }
+        if (tid == 0 && A.lse) A.lse[(int64_t)c.b * A.q.heads + h0 + hd] = lse2 * 0.6931471805599453f;
+        if (__syncthreads_or(bad && lse2 == lse2) && warp == 0) decode_repair<X>(A, c.b, h0 + hd, lse2);
+    }
+    if (A.weight && mine < parts) {                           // (one unit per cache head)
+        const int32_t t0 = max(c.lo, from * TT), t1 = min(c.hi, (from + count) * TT);
+        const float* score = A.score + ((int64_t)c.b * A.q.heads + h0) * A.score_len;
+        float* weight = A.weight + c.b * A.ws[0] + g * A.ws[1];
+        for (int32_t t = t0 + lane; t < t1; t += 32) {
+            float sum = 0.0f;
+#pragma unroll 4
+            for (int hd = 0; hd < heads; ++hd) {
+                const float z = score[hd * A.score_len + t];
+                if (z != -INFINITY) sum += exp2_fast(z - s_lse2[hd]);
+            }
+            if (sum != 0.0f) weight[t] += sum;
+        }
+    }
+    cluster.sync();                                           // nobody leaves while its results are read
 }
 
 // What every token received, from the scores that decode_kernel kept: a warp takes a span of tiles of the batch, in the order (sequence,
@@ -1003,16 +1149,18 @@ __global__ void __launch_bounds__(256) decode_weight_kernel(const __grid_constan
     long long pos = w * span;
     const long long stop = min(pos + span, total);
     if (pos >= stop) return;
-    int32_t b = 0, last = A.n_seqs;                          // the sequence: tiles_before[b] * heads <= pos < tiles_before[b + 1] * heads
-    while (last - b > 1) {
-        const int32_t mid = b + (last - b) / 2;
-        if (A.tiles_before[mid] * A.c.n_heads <= pos) b = mid;
-        else last = mid;
+    // the sequence: tiles_before[b] * heads <= pos < tiles_before[b + 1] * heads, 32 places looked at side by side
+    int32_t b = 0;
+    for (int32_t width = A.n_seqs; width > 1;) {
+        const int32_t step = (width + 31) / 32;
+        const int32_t at = b + lane * step;
+        const unsigned le = __ballot_sync(FULL_MASK, lane * step < width && A.tiles_before[at] * A.c.n_heads <= pos);
+        const int k = 31 - __clz(le);                        // (lane 0 is always among them)
+        b += k * step;
+        width = min(step, width - k * step);
     }
     while (pos < stop) {
-        const long long t0 = A.tiles_before[b], tiles = A.tiles_before[b + 1] - t0;
-        if (tiles == 0) { ++b; continue; }
-        const long long in = pos - t0 * A.c.n_heads;
+        const long long t0 = A.tiles_before[b], tiles = A.tiles_before[b + 1] - t0, in = pos - t0 * A.c.n_heads;
         if (in >= tiles * A.c.n_heads) { ++b; continue; }
         const int32_t g = (int32_t)(in / tiles);
         const long long at = in - g * tiles, n = min(tiles - at, stop - pos);
@@ -1022,13 +1170,27 @@ __global__ void __launch_bounds__(256) decode_weight_kernel(const __grid_constan
         const float* score = A.score + ((int64_t)b * A.q.heads + g * A.group) * A.score_len;
         const float* norm = A.lse2 + (int64_t)b * A.q.heads + g * A.group;
         float* weight = A.weight + b * A.ws[0] + g * A.ws[1];
-        for (int32_t t = from + lane; t < to; t += 32) {
-            float sum = 0.0f;
-            for (int32_t i = 0; i < A.group; ++i) {
-                const float s = score[i * A.score_len + t], z = norm[i];
-                if (s != -INFINITY) sum += exp2_fast(s - z);      // (z is -inf only where every s is)
+        constexpr int DEEP = 4;                              // tokens per lane whose loads are in flight together
+        for (int32_t t = from; t < to; t += 32 * DEEP) {
+            float sum[DEEP], old[DEEP];
+#pragma unroll
+            for (int x = 0; x < DEEP; ++x) {
+                sum[x] = 0.0f;
+                old[x] = t + 32 * x + lane < to ? weight[t + 32 * x + lane] : 0.0f;
             }
-            if (sum != 0.0f) weight[t] += sum;
+#pragma unroll 2
+            for (int32_t i = 0; i < A.group; ++i) {
+                const float z = norm[i];
+                float s[DEEP];
+#pragma unroll
+                for (int x = 0; x < DEEP; ++x) s[x] = t + 32 * x + lane < to ? score[i * A.score_len + t + 32 * x + lane] : -INFINITY;
+#pragma unroll
+                for (int x = 0; x < DEEP; ++x)
+                    if (s[x] != -INFINITY) sum[x] += exp2_fast(s[x] - z);      // (z is -inf only where every s is)
+            }
+#pragma unroll
+            for (int x = 0; x < DEEP; ++x)
+                if (sum[x] != 0.0f) weight[t + 32 * x + lane] = old[x] + sum[x];
         }
         pos += n;
     }
@@ -1046,6 +1208,28 @@ DecodeSpace decode_space(int64_t n_seqs, int64_t heads, int64_t max_tokens, int6
     s.score_len = (max_tokens + 31) / 32 * 32;
     s.bytes = s.score + (weight ? up256(n_seqs * heads * s.score_len * 4) : 0);
     return s;
+}
+
+// More than 48 KB of dynamic shared memory has to be asked for, once per kernel and device.
+template <auto kernel> rt_status allow_smem(int bytes) {
+    static std::atomic<uint64_t> asked{0};
+    int dev = 0;
+    CK(cudaGetDevice(&dev));
+    const uint64_t bit = 1ull << (dev & 63);
+    if (asked.load(std::memory_order_relaxed) & bit) return RT_OK;
+    CK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    asked.fetch_or(bit, std::memory_order_relaxed);
+    return RT_OK;
+}
+
+template <typename... P> rt_status launch_cluster(void (*kernel)(P...), unsigned grid, unsigned threads, int ctas, size_t smem, cudaStream_t s, P... args) {
+    cudaLaunchConfig_t c = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = ctas; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    c.gridDim = dim3(grid); c.blockDim = dim3(threads); c.dynamicSmemBytes = smem; c.stream = s; c.attrs = at; c.numAttrs = 1;
+    CK(cudaLaunchKernelEx(&c, kernel, args...));
+    return RT_OK;
 }
 
 template <typename... P> rt_status launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, cudaStream_t s, P... args) {
@@ -1066,7 +1250,16 @@ template <class X> rt_status launch_decode(DecodeArgs& A, char* work, cudaStream
     const DecodeSpace W = decode_space(A.n_seqs, A.q.heads, A.max_tokens, A.warps, X::PART, A.weight != nullptr);
     A.tiles_before = (long long*)work; A.lse2 = (float*)(work + W.lse2); A.part = (float*)(work + W.part); A.score = (float*)(work + W.score);
     A.score_len = W.score_len;
-    CK(cudaFuncSetAttribute(decode_kernel<X>, cudaFuncAttributeMaxDynamicSharedMemorySize, X::SMEM));
+    const long long tiles = (A.max_tokens + X::TT - 1) / X::TT, units = (long long)A.n_seqs * A.units;
+    if (A.max_tokens <= KLPM_ROW_TOKENS && units * (tiles ? tiles : 1) <= (long long)KLPM_ROW_TILES * A.warps && (!A.weight || A.head_tiles == 1)) {
+        // CTAs of a cluster: until every warp has a tile or the GPU is full
+        int ctas = 1;
+        while (ctas < 8 && ctas * KLPM_ROW_WARPS < tiles && units * ctas * 2 <= KLPM_SMS * (X::CTAS / 2)) ctas *= 2;
+        constexpr int bytes = KLPM_ROW_WARPS * X::WARP_SMEM;
+        if (rt_status st = allow_smem<decode_row_kernel<X>>(bytes)) return st;
+        return launch_cluster(decode_row_kernel<X>, (unsigned)(units * ctas), KLPM_ROW_WARPS * 32, ctas, bytes, s, A, (int32_t)ctas);
+    }
+    if (rt_status st = allow_smem<decode_kernel<X>>(X::SMEM)) return st;
     decode_kernel<X><<<KLPM_SMS * X::CTAS, KLPM_DECODE_WARPS * 32, X::SMEM, s>>>(A);
     CK(cudaGetLastError());
     const int64_t rows = (int64_t)A.n_seqs * A.q.heads;
@@ -1306,14 +1499,8 @@ __global__ void __launch_bounds__(256) evict_copy_kernel(const EvictArgs A) {
 }
 
 template <int T, bool HELD> rt_status launch_select(const EvictArgs& A, int64_t rows, int ctas, size_t smem, cudaStream_t s) {
-    CK(cudaFuncSetAttribute(evict_select_kernel<T, HELD>, cudaFuncAttributeMaxDynamicSharedMemorySize, KLPM_EVICT_HELD * 4));
-    cudaLaunchConfig_t c = {};
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = ctas; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    c.gridDim = dim3((unsigned)(rows * ctas)); c.blockDim = dim3(T); c.dynamicSmemBytes = smem; c.stream = s; c.attrs = at; c.numAttrs = 1;
-    CK(cudaLaunchKernelEx(&c, evict_select_kernel<T, HELD>, A, (int32_t)ctas));
-    return RT_OK;
+    if (rt_status st = allow_smem<evict_select_kernel<T, HELD>>(KLPM_EVICT_HELD * 4)) return st;
+    return launch_cluster(evict_select_kernel<T, HELD>, (unsigned)(rows * ctas), T, ctas, smem, s, A, (int32_t)ctas);
 }
 
 }  // namespace

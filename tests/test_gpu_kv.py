@@ -220,7 +220,26 @@ def check_decode(c, q, table, lengths, scale=None, window=0, weight=True, **more
     assert ((got_lse.double() - lse).abs()[~none] <= lse_tol[~none]).all()
     if w is not None:
         assert ((w.double() - weight).abs() <= weight_tol).all()
+    # the same with room for many more tokens in the table (other kernels take it): lengths beyond the narrow one's end are cut off by hand
+    lengths = lengths.clamp(max=table.shape[1] * c.page_size)
+    wide = wide_table(table, c.page_size)
+    w2 = torch.rand(n, c.n_heads, wide.shape[1] * c.page_size, generator=g, device="cuda") if weight is not None else None
+    before = w2.clone() if w2 is not None else None
+    got2, lse2 = torch.full_like(got, 7.0), torch.full_like(got_lse, 7.0)
+    K().kv_decode(c, q, wide, lengths, got2, scale=scale, window=window, lse=lse2, weight=w2, **more)
+    assert ((got2.double() - out).abs() <= out_tol).all()
+    assert torch.equal(none, lse2 == -math.inf)
+    assert ((lse2.double() - lse).abs()[~none] <= lse_tol[~none]).all()
+    if w2 is not None:
+        k = table.shape[1] * c.page_size
+        assert torch.equal(w2[..., k:], before[..., k:])
+        added = (weight - torch.rand(n, c.n_heads, k, generator=gen(5), device="cuda").double())
+        assert ((w2[..., :k].double() - before[..., :k].double() - added).abs() <= weight_tol + 4 * U * w2[..., :k].double()).all()
     return got, got_lse, w
+
+
+def wide_table(table, page):
+    return torch.cat([table, torch.full((table.shape[0], 40_000 // page), -1, dtype=torch.int32, device="cuda")], 1)
 
 
 def tables(g, lengths, page, width=None, spare=3):
@@ -342,17 +361,21 @@ def test_decode_infinities_and_nan_in_what_is_attended_to():
     c.k[at(0, 13)] = -math.inf                  # a score of -inf: that token has no weight
     c.k[at(1, 13)] = math.nan
     c.v[at(2, 13)] = math.inf
-    w = torch.zeros(4, 1, 40, device="cuda")
-    out, lse = torch.empty_like(q), torch.empty(4, 2, device="cuda")
-    K().kv_decode(c, q, table, lens, out, lse=lse, weight=w)
-    assert w[0, 0, 13] == 0 and torch.isfinite(out[0]).all() and torch.isfinite(lse[0]).all()
-    assert abs(float(w[0].sum()) - 2) < 1e-4
-    assert torch.isnan(out[1]).all() and torch.isnan(lse[1]).all() and torch.isnan(w[1]).all()
-    assert (out[2] == math.inf).all() and torch.isfinite(lse[2]).all()
-    assert torch.isfinite(out[3]).all()
+    c.v[at(3, 2)][..., 7] = -math.inf           # one element only
+    for pages in (table, wide_table(table, 8)):
+        w = torch.zeros(4, 1, pages.shape[1] * 8, device="cuda")
+        out, lse = torch.empty_like(q), torch.empty(4, 2, device="cuda")
+        K().kv_decode(c, q, pages, lens, out, lse=lse, weight=w)
+        w = w[:, :, :40]
+        assert w[0, 0, 13] == 0 and torch.isfinite(out[0]).all() and torch.isfinite(lse[0]).all()
+        assert abs(float(w[0].sum()) - 2) < 1e-4
+        assert torch.isnan(out[1]).all() and torch.isnan(lse[1]).all() and torch.isnan(w[1]).all()
+        assert (out[2] == math.inf).all() and torch.isfinite(lse[2]).all()
+        assert (out[3, :, 7] == -math.inf).all() and torch.isfinite(out[3, :, :7]).all() and torch.isfinite(out[3, :, 8:]).all()
     c.k[at(3, 0)[0]] = -math.inf                # a whole sequence of scores of -inf: nothing to attend to
-    K().kv_decode(c, q, table, torch.full((4,), 8, dtype=torch.int32, device="cuda"), out, lse=lse)
-    assert (out[3] == 0).all() and (lse[3] == -math.inf).all()
+    for pages in (table, wide_table(table, 8)):
+        K().kv_decode(c, q, pages, torch.full((4,), 8, dtype=torch.int32, device="cuda"), out, lse=lse)
+        assert (out[3] == 0).all() and (lse[3] == -math.inf).all()
 
 
 def test_decode_strides_and_rows_that_start_anywhere():
