@@ -274,7 +274,7 @@ template <int TX, int TC> void launch_append(const AppendArgs& A, bool vec, unsi
 //     A unit is a cache head and up to 8 NT of its query heads.
 //   - Probabilities enter the second product as the sum of two 16-bit numbers (16 bits of precision or more), whose products go to the same
 //     sums.  f16 probabilities are scaled by 2^15 so that small ones keep their bits.  A bf16 query next to an 8-bit cache
-//     is split into two f16 numbers in the same way.
+//     becomes f16, times a power of two per head that brings its largest element next to 2^15: exact down to 2^-29 of that.
 // ------------------------------------------------------------------------------------------------
 struct DecodeArgs {
     CacheDev c;
@@ -283,6 +283,7 @@ struct DecodeArgs {
     int64_t table_stride;
     int32_t n_seqs, group, max_tokens, window;
     int32_t head_tiles, units;         // units of a cache head, of a sequence
+    int32_t q_words;                   // query rows may be read in words of 4 bytes
     float scale;
     float* lse;                        // nullable
     float* weight;                     // nullable
@@ -306,19 +307,19 @@ template <int TQ_, int TC_, int DP_, int NT_> struct Dec {
     static constexpr int TQ = TQ_, TC = TC_, DP = DP_, NT = NT_;
     static constexpr bool E8 = TC == KV_E4M3;
     static constexpr bool HALF = E8 || TC == KV_F16;           // the products are of f16, else of bf16
-    static constexpr bool QLO = E8 && TQ == KV_BF16;           // the query is split into two f16 numbers
+    static constexpr bool SCALED = E8 && TQ == KV_BF16;        // the query becomes f16
     static constexpr int ROW = DP * (E8 ? 1 : 2);              // bytes of a row in shared memory
     static constexpr int CH = ROW / 16;
     static constexpr int TT = (E8 ? DP <= 128 : DP <= 64) ? 32 : 16;
     static constexpr int TILE = TT * ROW;                      // bytes of a half tile: keys or values
-    static constexpr int CTAS = DP > 128 || NT > 1 ? 2 : QLO ? 3 : 4;      // per SM: what the registers leave room for
+    static constexpr int CTAS = DP > 128 || NT > 1 ? 2 : 4;      // per SM: what the registers leave room for
     static constexpr int FIT = 192 * 1024 / (CTAS * KLPM_DECODE_WARPS * TILE);
     static constexpr int RING = FIT < 6 ? FIT : 6;             // half tiles
     static constexpr int WARP_SMEM = RING * TILE;
     static constexpr int SMEM = KLPM_DECODE_WARPS * WARP_SMEM;
     static constexpr int HEADS = 8 * NT;
     static constexpr int PART = HEADS * (2 + DP);
-    static constexpr int QF = QLO ? 2 : 1;                     // numbers that a query element is the sum of
+    static constexpr int KS = DP / 16;                         // steps of the first product, tiles of the output
 };
 
 __device__ __forceinline__ void token_range(const DecodeArgs& A, int32_t b, int32_t* lo, int32_t* hi) {
@@ -480,11 +481,15 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
                 }
             }
         } else {
-            const int64_t mine = page < 0 ? -1 : page * s0 + at * s1;
+            const int64_t mine = page < 0 ? 0 : page * s0 + at * s1;
+            const bool full = __all_sync(FULL_MASK, lane >= TT || page >= 0);
+            const unsigned there = __ballot_sync(FULL_MASK, page >= 0);
 #pragma unroll
             for (int i = 0; i < TT / RPI; ++i) {
-                const int64_t off = __shfl_sync(FULL_MASK, mine, i * RPI + my_row);
-                if (my_ch < chunks) cp_async16(to + place<X, VALUE>(i * RPI + my_row, my_ch) * 16, off < 0 ? base : base + off, off < 0 ? 0 : 16);
+                const char* p = base + __shfl_sync(FULL_MASK, mine, i * RPI + my_row);
+                int bytes = 16;
+                if (!full) bytes = (there >> (i * RPI + my_row) & 1) << 4;
+                if (my_ch < chunks) cp_async16(to + place<X, VALUE>(i * RPI + my_row, my_ch) * 16, p, bytes);
             }
         }
         if (++slot_in == RING) slot_in = 0;
@@ -518,7 +523,7 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
     // where the lane's rows of an ldmatrix are: chunk c of row r lies at r * ROW + ((c ^ r) & 7 | c & ~7) * 16.  Keys: tokens 0-15, two chunks;
     // values: tokens 0-7 and 8-15 of two chunks
     const int kr = lane & 15, kc = lane >> 4, vr = (lane & 7) + ((lane >> 4) << 3), vc = (lane >> 3) & 1;
-    uint32_t qb[X::QF][NT][KS][2];
+    uint32_t qb[NT][KS][2];
     float coef[NT][2], m[NT][2], l[NT][2], o[NT][KS][4];
     bool fresh = true, begun_here = false;
     int32_t heads = 0;
@@ -545,41 +550,43 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const bool have = n * 8 + r8 < heads;
-                const Q* q = reinterpret_cast<const Q*>(qp + (n * 8 + r8) * A.q.sh);
-                float up = 1.0f, c = A.scale * A.c.k_scale * log2e;
-                if constexpr (X::QLO) {
-                    // a power of two brings the largest element next to 2^15: f16 pairs then hold elements down to 2^-39 of it exactly
+                const uint16_t* q = reinterpret_cast<const uint16_t*>(qp + (n * 8 + r8) * A.q.sh);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        const int d = q_element<X>(ks, j, part);
+                        qb[n][ks][part] = !have || d >= A.c.dim ? 0u : A.q_words ? __ldg(reinterpret_cast<const uint32_t*>(q + d))
+                                                                                : __ldg(q + d) | (uint32_t)__ldg(q + d + 1) << 16;
+                    }
+                float c = A.scale * A.c.k_scale * log2e;
+                if constexpr (X::SCALED) {
                     float most = 0.0f;
-                    if (have)
-                        for (int d = j; d < A.c.dim; d += 4) {
-                            const float x = fabsf(to_float(q[d]));
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                        for (int part = 0; part < 2; ++part) {
+                            const float x = fabsf(__uint_as_float(qb[n][ks][part] << 16)), y = fabsf(__uint_as_float(qb[n][ks][part] & 0xffff0000u));
                             if (x < INFINITY) most = fmaxf(most, x);
+                            if (y < INFINITY) most = fmaxf(most, y);
                         }
                     most = fmaxf(most, __shfl_xor_sync(FULL_MASK, most, 1));
                     most = fmaxf(most, __shfl_xor_sync(FULL_MASK, most, 2));
                     int e = 0;
                     if (most > 0.0f) frexpf(most, &e);
                     e = max(-110, min(110, 15 - e));
-                    up = ldexpf(1.0f, e);
+                    const float up = ldexpf(1.0f, e);
                     c = ldexpf(c, -e);
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                        for (int part = 0; part < 2; ++part) {
+                            const __half2 h = __floats2half2_rn(__uint_as_float(qb[n][ks][part] << 16) * up, __uint_as_float(qb[n][ks][part] & 0xffff0000u) * up);
+                            qb[n][ks][part] = *reinterpret_cast<const uint32_t*>(&h);
+                        }
                 }
                 coef[n][0] = __shfl_sync(FULL_MASK, c, 8 * j);           // of heads 2j and 2j+1
                 coef[n][1] = __shfl_sync(FULL_MASK, c, 8 * j + 4);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                    for (int part = 0; part < 2; ++part) {
-                        const int d = q_element<X>(ks, j, part);
-                        const float x = have && d < A.c.dim ? to_float(q[d]) * up : 0.0f, y = have && d + 1 < A.c.dim ? to_float(q[d + 1]) * up : 0.0f;
-                        uint32_t lo;
-                        split2<X::HALF>(x, y, &qb[0][n][ks][part], &lo);
-                        if constexpr (X::QLO) {
-                            // (an infinite element minus itself would be NaN: its second half is 0)
-                            if (isinf(x)) lo &= 0xffff0000u;
-                            if (isinf(y)) lo &= 0x0000ffffu;
-                            qb[X::QF - 1][n][ks][part] = lo;
-                        }
-                    }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.0f; }
 #pragma unroll
@@ -597,9 +604,7 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
             for (int t = 0; t < TN; ++t) s[n][t][0] = s[n][t][1] = s[n][t][2] = s[n][t][3] = 0.0f;
         auto kq = [&](int t, int ks, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int f = 0; f < X::QF; ++f) mma16816<X::HALF>(s[n][t], a0, a1, a2, a3, qb[f][n][ks][0], qb[f][n][ks][1]);
+            for (int n = 0; n < NT; ++n) mma16816<X::HALF>(s[n][t], a0, a1, a2, a3, qb[n][ks][0], qb[n][ks][1]);
         };
         if constexpr (X::E8) {
 #pragma unroll
@@ -633,18 +638,28 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
         // p = 2^(s - m): tokens r8 and r8 + 8 of heads 2j and 2j + 1
         const unsigned have = s_there[tile_out++ & 7];
         uint32_t ph[NT][TN][2], pl[NT][TN][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[n][t][i] *= coef[n][i & 1];
+        if (have != (TT == 32 ? 0xffffffffu : 0xffffu)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int t = 0; t < TN; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!((have >> (t * 16 + (i >> 1) * 8 + r8)) & 1)) s[n][t][i] = -INFINITY;
+        }
         bool grown = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int t = 0; t < TN; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float& z = s[n][t][i];
-                    z *= coef[n][i & 1];
-                    if (have != (TT == 32 ? 0xffffffffu : 0xffffu) && !((have >> (t * 16 + (i >> 1) * 8 + r8)) & 1)) z = -INFINITY;
-                    grown |= z > m[n][i & 1];
-                }
+                for (int i = 0; i < 4; ++i) grown |= s[n][t][i] > m[n][i & 1];
         if (A.weight) {
             const int32_t g = cc.u / A.head_tiles, h0 = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS;
             float* row = A.score + ((int64_t)cc.b * A.q.heads + h0) * A.score_len + (int64_t)cc.tile * TT + r8;
@@ -772,28 +787,166 @@ template <class X> __device__ __forceinline__ void clear_ring(const DecodeArgs& 
     if (A.c.dim * (X::E8 ? 1 : 2) / 16 < X::CH)
         for (int i = threadIdx.x; i < bytes / 16; i += blockDim.x) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
 }
-// A row's result, where a warp has all of it.
-template <class X> __device__ __forceinline__ void write_part(float* part, int32_t heads, const float (&m)[X::NT][2], const float (&l)[X::NT][2],
-                                                              const float (&o)[X::NT][X::DP / 16][4], int32_t dim) {
+// What a warp has of a row, as its registers hold it: m and sums of the heads, then per (8 heads, 16 elements) a float4 per lane -- elements r8,
+// r8 + 8 of the tile for heads 2j, 2j + 1.
+template <class X> __device__ __forceinline__ void write_part(float* part, const float (&m)[X::NT][2], const float (&l)[X::NT][2], const float (&o)[X::NT][X::KS][4]) {
+    const int lane = threadIdx.x & 31, j = lane & 3;
+#pragma unroll
+    for (int n = 0; n < X::NT; ++n) {
+        if (lane < 4) {
+            *reinterpret_cast<float2*>(part + n * 8 + 2 * j) = make_float2(m[n][0], m[n][1]);
+            *reinterpret_cast<float2*>(part + X::HEADS + n * 8 + 2 * j) = make_float2(l[n][0], l[n][1]);
+        }
+#pragma unroll
+        for (int x = 0; x < X::KS; ++x)
+            reinterpret_cast<float4*>(part + 2 * X::HEADS)[(n * X::KS + x) * 32 + lane] = make_float4(o[n][x][0], o[n][x][1], o[n][x][2], o[n][x][3]);
+    }
+}
+// The parts of a row joined for output tile x, by a warp: lane 4 r8 + j has elements r8, r8 + 8 of heads 2j, 2j + 1 of each group of eight.
+template <class X> struct Joined {
+    float m[X::NT][2], l[X::NT][2], o[X::NT][4];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int n = 0; n < X::NT; ++n) {
+            m[n][0] = m[n][1] = -INFINITY;
+            l[n][0] = l[n][1] = o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
+        }
+    }
+    // parts k0, k0 + step, ... below parts; DEEP of them in flight together.  part(k): where part k is.
+    template <int DEEP, class G> __device__ __forceinline__ void add(int x, int32_t k0, int32_t step, int32_t parts, G part) {
+        const int lane = threadIdx.x & 31, j = lane & 3;
+        for (; k0 < parts; k0 += step * DEEP) {
+            float2 pm[DEEP][X::NT], pl[DEEP][X::NT];
+            float4 po[DEEP][X::NT];
+#pragma unroll
+            for (int y = 0; y < DEEP; ++y) {
+                const bool some = k0 + y * step < parts;
+                const float* p = part(some ? k0 + y * step : k0);
+#pragma unroll
+                for (int n = 0; n < X::NT; ++n) {
+                    pm[y][n] = *reinterpret_cast<const float2*>(p + n * 8 + 2 * j);
+                    pl[y][n] = *reinterpret_cast<const float2*>(p + X::HEADS + n * 8 + 2 * j);
+                    po[y][n] = reinterpret_cast<const float4*>(p + 2 * X::HEADS)[(n * X::KS + x) * 32 + lane];
+                    if (!some) { pm[y][n] = make_float2(-INFINITY, -INFINITY); pl[y][n] = make_float2(0, 0); po[y][n] = make_float4(0, 0, 0, 0); }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < X::NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float top = m[n][e];
+#pragma unroll
+                    for (int y = 0; y < DEEP; ++y) top = fmaxf(top, e ? pm[y][n].y : pm[y][n].x);
+                    const float base = top == -INFINITY ? 0.0f : top, f = exp2_fast(m[n][e] - base);
+                    m[n][e] = top;
+                    l[n][e] *= f; o[n][e] *= f; o[n][e + 2] *= f;
+#pragma unroll
+                    for (int y = 0; y < DEEP; ++y) {
+                        const float pf = exp2_fast((e ? pm[y][n].y : pm[y][n].x) - base);
+                        l[n][e] += pf * (e ? pl[y][n].y : pl[y][n].x);
+                        o[n][e] += pf * (e ? po[y][n].y : po[y][n].x);
+                        o[n][e + 2] += pf * (e ? po[y][n].w : po[y][n].z);
+                    }
+                }
+        }
+    }
+    // to shared memory and, of what `others` warps have left there, back again
+    __device__ __forceinline__ void put(float4* at) const {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int n = 0; n < X::NT; ++n) {
+            at[(n * 2) * 32 + lane] = make_float4(m[n][0], m[n][1], l[n][0], l[n][1]);
+            at[(n * 2 + 1) * 32 + lane] = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
+        }
+    }
+    __device__ __forceinline__ void take(const float4* all, int others) {
+        const int lane = threadIdx.x & 31;
+        clear();
+        for (int w = 0; w < others; ++w)
+#pragma unroll
+            for (int n = 0; n < X::NT; ++n) {
+                const float4 a = all[(w * X::NT * 2 + n * 2) * 32 + lane], b = all[(w * X::NT * 2 + n * 2 + 1) * 32 + lane];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float pm = e ? a.y : a.x, top = fmaxf(m[n][e], pm), base = top == -INFINITY ? 0.0f : top;
+                    const float f = exp2_fast(m[n][e] - base), pf = exp2_fast(pm - base);
+                    m[n][e] = top;
+                    l[n][e] = l[n][e] * f + pf * (e ? a.w : a.z);
+                    o[n][e] = o[n][e] * f + pf * (e ? b.y : b.x);
+                    o[n][e + 2] = o[n][e + 2] * f + pf * (e ? b.w : b.z);
+                }
+            }
+    }
+};
+// Elements of an output tile that came out as NaN although the scores are numbers, by one warp: an infinite value times the second half of
+// a probability, which may be 0 or negative, is no number, while the sum of p_t v_t is infinite.  They are summed with whole
+// probabilities, one token after the other.
+template <class X> __device__ __noinline__ void decode_repair(const DecodeArgs& A, int32_t b, int32_t h, int x, float lse2) {
+    using Q = typename Elem<X::TQ>::T;
+    using C = typename Elem<X::TC>::T;
+    const int lane = threadIdx.x & 31;
+    const int32_t g = h / A.group;
+    const int d = out_element<X>(x, lane & 7, (lane >> 3) & 1);             // of lanes 0-15
+    const Q* q = reinterpret_cast<const Q*>(A.q.p + b * A.q.sr + h * A.q.sh);
+    Q* out = reinterpret_cast<Q*>(A.out.p + b * A.out.sr + h * A.out.sh);
+    float o = 0.0f;
+    int32_t lo, hi;
+    token_range(A, b, &lo, &hi);
+    for (int32_t t = lo; t < hi; ++t) {
+        const int32_t page = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
+        if ((unsigned)page >= (unsigned)A.c.n_pages) continue;
+        const int32_t at = t & ((1 << A.c.page_shift) - 1);
+        const C* k = reinterpret_cast<const C*>(A.c.k + page * A.c.ks[0] + at * A.c.ks[1] + g * A.c.ks[2]);
+        const C* v = reinterpret_cast<const C*>(A.c.v + page * A.c.vs[0] + at * A.c.vs[1] + g * A.c.vs[2]);
+        float s = 0.0f;
+        for (int i = lane; i < A.c.dim; i += 32) s += to_float(q[i]) * to_float(k[i]);
+        for (int w = 16; w; w >>= 1) s += __shfl_xor_sync(FULL_MASK, s, w);
+        s *= A.scale * A.c.k_scale * 1.4426950408889634f;
+        if (s != -INFINITY && d < A.c.dim) o += exp2f(s - lse2) * to_float(v[d]);
+    }
+    __syncwarp();
+    if (lane < 16 && d < A.c.dim && to_float(out[d]) != to_float(out[d])) out[d] = from_float<Q>(o * A.c.v_scale);
+}
+// The outputs of tile x of a unit whose parts are joined; what a warp writes here nobody else writes.
+template <class X> __device__ __forceinline__ void write_joined(const DecodeArgs& A, const Joined<X>& J, int32_t b, int32_t h0, int32_t heads, int x) {
+    using Q = typename Elem<X::TQ>::T;
     const int lane = threadIdx.x & 31, r8 = lane >> 2, j = lane & 3;
+    unsigned bad = 0;                                        // heads with a NaN among this lane's elements
 #pragma unroll
     for (int n = 0; n < X::NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int hd = n * 8 + 2 * j + e;
             if (hd >= heads) continue;
-            if (r8 == 0) { part[hd] = m[n][e]; part[X::HEADS + hd] = l[n][e]; }
-            float* y = part + 2 * X::HEADS + hd * X::DP;
+            const float sum = J.l[n][e], f = sum == 0.0f ? 0.0f : A.c.v_scale / sum;
+            Q* out = reinterpret_cast<Q*>(A.out.p + b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
 #pragma unroll
-            for (int x = 0; x < X::DP / 16; ++x)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int d = out_element<X>(x, r8, i);
-                    if (d < dim) y[d] = o[n][x][i * 2 + e];
-                }
+            for (int i = 0; i < 2; ++i) {
+                const int d = out_element<X>(x, r8, i);
+                const float y = sum == 0.0f ? 0.0f : J.o[n][i * 2 + e] * f;
+                if (d < A.c.dim) out[d] = from_float<Q>(y);
+                if (d < A.c.dim && y != y && sum == sum) bad |= 1u << hd;
+            }
+            if (x == 0 && r8 == 0) {
+                const int64_t row = (int64_t)b * A.q.heads + h0 + hd;
+                const float y = sum == 0.0f ? -INFINITY : J.m[n][e] + log2f(sum);
+                if (A.lse) A.lse[row] = y * 0.6931471805599453f;
+                A.lse2[row] = y;
+            }
         }
+    bad = __reduce_or_sync(FULL_MASK, bad);
+    while (bad) {
+        const int hd = __ffs(bad) - 1;
+        bad &= bad - 1;
+        float y = 0.0f;
+#pragma unroll
+        for (int n = 0; n < X::NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (n * 8 + e == (hd & 9)) y = J.m[n][e] + log2f(J.l[n][e]);
+        decode_repair<X>(A, b, h0 + hd, x, __shfl_sync(FULL_MASK, y, (hd & 7) >> 1));
+    }
 }
-
 
 template <class X>
 __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel(const __grid_constant__ DecodeArgs A) {
@@ -863,7 +1016,7 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
     decode_span<X>(A, smem_addr(smem) + warp * X::WARP_SMEM, s_there[warp], ci, min(span, total - pos),
                    [&](const Cursor<X>& cc, bool begun, bool ended, int32_t heads, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[NT][KS][4]) {
         if (!begun || !ended) {
-            write_part<X>(A.part + ((int64_t)w * 2 + (first_piece ? 0 : 1)) * X::PART, heads, m, l, o, A.c.dim);
+            write_part<X>(A.part + ((int64_t)w * 2 + (first_piece ? 0 : 1)) * X::PART, m, l, o);
         } else {
             const int r8 = lane >> 2, j = lane & 3;
             const int32_t g = cc.u / A.head_tiles, h0 = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS;
@@ -895,139 +1048,45 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
     });
 }
 
-// Elements of a row that came out as NaN although its scores are numbers, by one warp: an infinite value times the second half of a
-// probability, which may be 0 or negative, is no number, while the sum of p_t v_t is infinite.  They are summed with whole
-// probabilities, one token after the other.
-template <class X> __device__ __noinline__ void decode_repair(const DecodeArgs& A, int32_t b, int32_t h, float lse2) {
-    using Q = typename Elem<X::TQ>::T;
-    using C = typename Elem<X::TC>::T;
-    constexpr int PER = X::DP / 32;
-    const int lane = threadIdx.x & 31;
-    const int32_t g = h / A.group;
-    const Q* q = reinterpret_cast<const Q*>(A.q.p + b * A.q.sr + h * A.q.sh);
-    Q* out = reinterpret_cast<Q*>(A.out.p + b * A.out.sr + h * A.out.sh);
-    float o[PER];
-#pragma unroll
-    for (int x = 0; x < PER; ++x) o[x] = 0.0f;
-    int32_t lo, hi;
-    token_range(A, b, &lo, &hi);
-    for (int32_t t = lo; t < hi; ++t) {
-        const int32_t page = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
-        if ((unsigned)page >= (unsigned)A.c.n_pages) continue;
-        const int32_t at = t & ((1 << A.c.page_shift) - 1);
-        const C* k = reinterpret_cast<const C*>(A.c.k + page * A.c.ks[0] + at * A.c.ks[1] + g * A.c.ks[2]);
-        const C* v = reinterpret_cast<const C*>(A.c.v + page * A.c.vs[0] + at * A.c.vs[1] + g * A.c.vs[2]);
-        float s = 0.0f;
-        for (int d = lane; d < A.c.dim; d += 32) s += to_float(q[d]) * to_float(k[d]);
-        for (int w = 16; w; w >>= 1) s += __shfl_xor_sync(FULL_MASK, s, w);
-        s *= A.scale * A.c.k_scale * 1.4426950408889634f;
-        if (s == -INFINITY) continue;
-        const float p = exp2f(s - lse2);
-#pragma unroll
-        for (int x = 0; x < PER; ++x)
-            if (lane + 32 * x < A.c.dim) o[x] += p * to_float(v[lane + 32 * x]);
-    }
-#pragma unroll
-    for (int x = 0; x < PER; ++x)
-        if (lane + 32 * x < A.c.dim && to_float(out[lane + 32 * x]) != to_float(out[lane + 32 * x])) out[lane + 32 * x] = from_float<Q>(o[x] * A.c.v_scale);
-}
-template <class X> __device__ __forceinline__ void decode_check(const DecodeArgs& A, int32_t b, int32_t h, float lse2) {
-    using Q = typename Elem<X::TQ>::T;
-    const Q* out = reinterpret_cast<const Q*>(A.out.p + b * A.out.sr + h * A.out.sh);
-    bool bad = false;
-    for (int d = threadIdx.x & 31; d < A.c.dim; d += 32) bad |= to_float(out[d]) != to_float(out[d]);
-    if (__any_sync(FULL_MASK, bad) && lse2 == lse2) decode_repair<X>(A, b, h, lse2);
-}
-
-// Rows that were cut into parts, and rows with nothing to attend to.  WPR = 8: a CTA per row (sequence, query head), where few rows have
-// many parts each.  WPR = 1: a warp per row, where many rows have few.
+// Rows that were cut into parts, and rows with nothing to attend to.  An item is 16 elements of a unit.  WPR = 8: a CTA per item, where few
+// rows have many parts each.  WPR = 1: a warp per item, where many rows have few.
 template <class X, int WPR>
 __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant__ DecodeArgs A) {
     using Q = typename Elem<X::TQ>::T;
-    constexpr int PER = X::DP / 32;
-    __shared__ float s_m[8], s_l[8], s_o[WPR == 8 ? 8 : 1][X::DP];
+    __shared__ float4 s_all[WPR == 8 ? 8 * X::NT * 2 * 32 : 1];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t row = WPR == 8 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + warp;
-    if (row >= (int64_t)A.n_seqs * A.q.heads) return;
-    const int32_t b = (int32_t)(row / A.q.heads), h = (int32_t)(row % A.q.heads), g = h / A.group, i = h - g * A.group;
-    const int32_t u = g * A.head_tiles + i / X::HEADS, hd = i % X::HEADS;
+    const int64_t item = WPR == 8 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + warp, row = item / X::KS;
+    const int x = (int)(item % X::KS);
+    if (row >= (int64_t)A.n_seqs * A.units) return;
+    const int32_t b = (int32_t)(row / A.units), u = (int32_t)(row % A.units), g = u / A.head_tiles, in = (u - g * A.head_tiles) * X::HEADS;
+    const int32_t h0 = g * A.group + in, heads = min(X::HEADS, A.group - in);
     const long long t0 = A.tiles_before[b], tiles = A.tiles_before[b + 1] - t0;
     const long long span = span_of(A.tiles_before[A.n_seqs] * A.units, A.warps);
     const long long R = t0 * A.units + u * tiles, E = R + tiles;
     const int32_t w0 = (int32_t)(R / span), parts = tiles > 0 ? (int32_t)((E - 1) / span) - w0 + 1 : 0;
-    if (parts == 1) {                                        // decode_kernel has written it
-        if (WPR == 1 || warp == 0) decode_check<X>(A, b, h, A.lse2[row]);
+    if (parts == 1) {                                        // decode_kernel has written it; is there anything to repair?
+        if (WPR == 8 && warp) return;
+        const int d = out_element<X>(x, lane & 7, (lane >> 3) & 1);
+        for (int32_t hd = 0; hd < heads; ++hd) {
+            const Q* out = reinterpret_cast<const Q*>(A.out.p + b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
+            const float lse2 = A.lse2[(int64_t)b * A.q.heads + h0 + hd], y = d < A.c.dim ? to_float(out[d]) : 0.0f;
+            if (__any_sync(FULL_MASK, y != y) && lse2 == lse2) decode_repair<X>(A, b, h0 + hd, x, lse2);
+        }
         return;
     }
     const int first = w0 * span == R ? 0 : 1;
-    auto part = [&](int k) -> const float* { return A.part + ((int64_t)(w0 + k) * 2 + (k == 0 ? first : 0)) * X::PART; };
-    float m = -INFINITY, l = 0.0f, o[PER];
-#pragma unroll
-    for (int x = 0; x < PER; ++x) o[x] = 0.0f;
-    constexpr int DEEP = 4;                                  // parts of a warp whose loads are in flight together
-    for (int32_t k0 = WPR == 8 ? warp : 0; k0 < parts; k0 += WPR * DEEP) {
-        float pm[DEEP], pl[DEEP], v[DEEP][PER];
-#pragma unroll
-        for (int y = 0; y < DEEP; ++y) {
-            const bool some = k0 + y * WPR < parts;
-            const float* p = part(some ? k0 + y * WPR : k0);
-            pm[y] = some ? p[hd] : -INFINITY;
-            pl[y] = some ? p[X::HEADS + hd] : 0.0f;
-#pragma unroll
-            for (int x = 0; x < PER; ++x) v[y][x] = some && lane + 32 * x < A.c.dim ? p[2 * X::HEADS + hd * X::DP + lane + 32 * x] : 0.0f;
-        }
-        float top = m;
-#pragma unroll
-        for (int y = 0; y < DEEP; ++y) top = fmaxf(top, pm[y]);
-        const float base = top == -INFINITY ? 0.0f : top, f = exp2_fast(m - base);
-        m = top;
-        l *= f;
-#pragma unroll
-        for (int x = 0; x < PER; ++x) o[x] *= f;
-#pragma unroll
-        for (int y = 0; y < DEEP; ++y) {
-            const float pf = exp2_fast(pm[y] - base);
-            l += pl[y] * pf;
-#pragma unroll
-            for (int x = 0; x < PER; ++x) o[x] += v[y][x] * pf;
-        }
-    }
+    Joined<X> J;
+    J.clear();
+    J.template add<4>(x, WPR == 8 ? warp : 0, WPR, parts, [&](int k) { return A.part + ((int64_t)(w0 + k) * 2 + (k == 0 ? first : 0)) * X::PART; });
     if constexpr (WPR == 8) {
-        if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
-#pragma unroll
-        for (int x = 0; x < PER; ++x) s_o[warp][lane + 32 * x] = o[x];
+        J.put(s_all + warp * X::NT * 2 * 32);
         __syncthreads();
         if (warp) return;
-        for (int k = 0; k < 8; ++k) m = fmaxf(m, s_m[k]);
-        const float base = m == -INFINITY ? 0.0f : m;
-        l = 0.0f;
-#pragma unroll
-        for (int x = 0; x < PER; ++x) o[x] = 0.0f;
-        for (int k = 0; k < 8; ++k) {
-            const float f = exp2_fast(s_m[k] - base);
-            l += s_l[k] * f;
-#pragma unroll
-            for (int x = 0; x < PER; ++x) o[x] += s_o[k][lane + 32 * x] * f;
-        }
+        J.take(s_all, 8);
     }
-    Q* out = reinterpret_cast<Q*>(A.out.p + b * A.out.sr + h * A.out.sh);
-    const float f = l == 0.0f ? 0.0f : A.c.v_scale / l;
-    bool bad = false;
-#pragma unroll
-    for (int x = 0; x < PER; ++x)
-        if (lane + 32 * x < A.c.dim) {
-            const float z = l == 0.0f ? 0.0f : o[x] * f;
-            out[lane + 32 * x] = from_float<Q>(z);
-            bad |= z != z;
-        }
-    const float y = l == 0.0f ? -INFINITY : m + log2f(l);
-    if (lane == 0) {
-        if (A.lse) A.lse[row] = y * 0.6931471805599453f;
-        A.lse2[row] = y;
-    }
-    if (__any_sync(FULL_MASK, bad) && y == y) decode_repair<X>(A, b, h, y);
+    write_joined<X>(A, J, b, h0, heads, x);
 }
 
 // Small calls: a cluster of CTAs per row (sequence, unit), its tiles dealt out to all of the cluster's warps, whose results are joined through
@@ -1036,11 +1095,12 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
 template <class X>
 __global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_kernel(const __grid_constant__ DecodeArgs A, int32_t ctas) {
     using Q = typename Elem<X::TQ>::T;
-    constexpr int TT = X::TT, KS = X::DP / 16, NT = X::NT, MOST = 8 * KLPM_ROW_WARPS;
+    constexpr int TT = X::TT, KS = X::KS, NT = X::NT;
     static_assert(X::PART * 4 <= X::WARP_SMEM, "a warp's result lies in its ring");
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ unsigned s_there[KLPM_ROW_WARPS][8];
-    __shared__ float s_f[X::HEADS][MOST], s_lse2[X::HEADS], s_scale[X::HEADS], s_o[KLPM_ROW_WARPS * 32];
+    __shared__ float4 s_all[KLPM_ROW_WARPS * NT * 2 * 32];
+    __shared__ float s_lse2[X::HEADS];
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int32_t rank = blockIdx.x % ctas, row = blockIdx.x / ctas;
@@ -1056,7 +1116,6 @@ __global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_k
     clear_ring<X>(A, smem, KLPM_ROW_WARPS * X::WARP_SMEM);
     __syncthreads();
     const int32_t mine = warp * ctas + rank;                  // neighbouring parts on different SMs
-    float* part = reinterpret_cast<float*>(smem + warp * X::WARP_SMEM);
     const int32_t from = c.first + mine * per, count = min(per, c.end - from);
     if (mine < parts) {
         c.tile = from;
@@ -1064,64 +1123,45 @@ __global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_k
                        [&](const Cursor<X>&, bool, bool, int32_t, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[NT][KS][4]) {
             cp_async_wait<0>();
             __syncwarp();
-            write_part<X>(part, heads, m, l, o, A.c.dim);
+            write_part<X>(reinterpret_cast<float*>(smem + warp * X::WARP_SMEM), m, l, o);
         });
     }
     cluster.sync();
-    // the factor of every part, and the sum, of every head
-    for (int hd = warp; hd < heads; hd += KLPM_ROW_WARPS) {
-        float pm[MOST / 32], m = -INFINITY, l = 0.0f;
-#pragma unroll
-        for (int i = 0; i < MOST / 32; ++i) {
-            const int k = lane + 32 * i;
-            pm[i] = k < parts ? reinterpret_cast<const float*>(cluster.map_shared_rank(smem, k % ctas) + k / ctas * X::WARP_SMEM)[hd] : -INFINITY;
-            m = fmaxf(m, pm[i]);
+    // output tiles: where parts are few, one per warp of the cluster; else one per CTA at a time, the parts shared by its warps
+    auto part = [&](int k) { return reinterpret_cast<const float*>(cluster.map_shared_rank(smem, k % ctas) + k / ctas * X::WARP_SMEM); };
+    Joined<X> J;
+    if (parts <= 16) {
+        for (int x = mine; x < KS; x += warps) {
+            J.clear();
+            J.template add<4>(x, 0, 1, parts, part);
+            write_joined<X>(A, J, c.b, h0, heads, x);
         }
-        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL_MASK, m, d));
-        const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int i = 0; i < MOST / 32; ++i) {
-            const int k = lane + 32 * i;
-            if (k >= parts) continue;
-            const float f = exp2_fast(pm[i] - base);
-            l += f * reinterpret_cast<const float*>(cluster.map_shared_rank(smem, k % ctas) + k / ctas * X::WARP_SMEM)[X::HEADS + hd];
-            s_f[hd][k] = f;
-        }
-        for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(FULL_MASK, l, d);
-        if (lane == 0) {
-            s_lse2[hd] = l == 0.0f ? -INFINITY : m + log2f(l);
-            s_scale[hd] = l == 0.0f ? 0.0f : A.c.v_scale / l;
+    } else {
+        for (int x = rank; x < KS; x += ctas) {
+            J.clear();
+            J.template add<4>(x, warp, KLPM_ROW_WARPS, parts, part);
+            J.put(s_all + warp * NT * 2 * 32);
+            __syncthreads();
+            if (warp == 0) {
+                J.take(s_all, KLPM_ROW_WARPS);
+                write_joined<X>(A, J, c.b, h0, heads, x);
+            }
+            __syncthreads();
         }
     }
-    __syncthreads();
-    // outputs: a head per CTA at a time, an element per thread, the parts shared by the threads that are left
-    constexpr int SLICES = KLPM_ROW_WARPS * 32 / X::DP;
-    const int d = tid % X::DP, slice = tid / X::DP;
-    for (int hd = rank; hd < heads; hd += ctas) {
-        float y = 0.0f;
-        if (d < A.c.dim) {
-#pragma unroll 4
-            for (int k = slice; k < parts; k += SLICES)
-                y += s_f[hd][k] * reinterpret_cast<const float*>(cluster.map_shared_rank(smem, k % ctas) + k / ctas * X::WARP_SMEM)[2 * X::HEADS + hd * X::DP + d];
+    if (A.weight) {                                           // (one unit per cache head)
+        for (int hd = warp; hd < heads; hd += KLPM_ROW_WARPS) {
+            float m = -INFINITY, l = 0.0f;
+            for (int k = lane; k < parts; k += 32) m = fmaxf(m, part(k)[hd]);
+            for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL_MASK, m, d));
+            const float base = m == -INFINITY ? 0.0f : m;
+            for (int k = lane; k < parts; k += 32) l += exp2_fast(part(k)[hd] - base) * part(k)[X::HEADS + hd];
+            for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(FULL_MASK, l, d);
+            if (lane == 0) s_lse2[hd] = l == 0.0f ? -INFINITY : m + log2f(l);
         }
-        if (SLICES > 1) {
-            __syncthreads();
-            s_o[tid] = y;
-            __syncthreads();
-            if (slice == 0)
-                for (int i = 1; i < SLICES; ++i) y += s_o[i * X::DP + d];
-        }
-        const float lse2 = s_lse2[hd];
-        bool bad = false;
-        if (slice == 0 && d < A.c.dim) {
-            y = lse2 == -INFINITY ? 0.0f : y * s_scale[hd];
-            reinterpret_cast<Q*>(A.out.p + c.b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh)[d] = from_float<Q>(y);
-            bad = y != y;
-        }
-        if (tid == 0 && A.lse) A.lse[(int64_t)c.b * A.q.heads + h0 + hd] = lse2 * 0.6931471805599453f;
-        if (__syncthreads_or(bad && lse2 == lse2) && warp == 0) decode_repair<X>(A, c.b, h0 + hd, lse2);
+        __syncthreads();
     }
-    if (A.weight && mine < parts) {                           // (one unit per cache head)
+    if (A.weight && mine < parts) {
         const int32_t t0 = max(c.lo, from * TT), t1 = min(c.hi, (from + count) * TT);
         const float* score = A.score + ((int64_t)c.b * A.q.heads + h0) * A.score_len;
         float* weight = A.weight + c.b * A.ws[0] + g * A.ws[1];
@@ -1262,18 +1302,18 @@ template <class X> rt_status launch_decode(DecodeArgs& A, char* work, cudaStream
     if (rt_status st = allow_smem<decode_kernel<X>>(X::SMEM)) return st;
     decode_kernel<X><<<KLPM_SMS * X::CTAS, KLPM_DECODE_WARPS * 32, X::SMEM, s>>>(A);
     CK(cudaGetLastError());
-    const int64_t rows = (int64_t)A.n_seqs * A.q.heads;
-    // a row has 1184 / rows parts or so: with fewer rows than that, eight warps share a row's
-    rt_status st = rows <= A.warps ? launch_after(decode_join_kernel<X, 8>, dim3((unsigned)rows), 256, s, A)
-                                   : launch_after(decode_join_kernel<X, 1>, dim3((unsigned)((rows + 7) / 8)), 256, s, A);
+    // a unit has A.warps / units parts or so: with more than a few of them, eight warps share them
+    const int64_t items = units * X::KS;
+    if (items > 0x7fffffffLL) return RT_ERR_TOO_LARGE;
+    rt_status st = units * 4 <= A.warps ? launch_after(decode_join_kernel<X, 8>, dim3((unsigned)items), 256, s, A)
+                                        : launch_after(decode_join_kernel<X, 1>, dim3((unsigned)((items + 7) / 8)), 256, s, A);
     if (st || !A.weight) return st;
     return launch_after(decode_weight_kernel<X::TT>, dim3(KLPM_SMS * 4), 256, s, A);
 }
 
-// The instance for a call: DP = dim rounded up to 64, 128 or 256, 8 or 16 query heads per unit.  (16 where the registers hold them: not for wide
-// heads, and not where the query is kept as two numbers.)
+// The instance for a call: DP = dim rounded up to 64, 128 or 256, 8 or 16 query heads per unit (8 for wide heads: the registers).
 template <int TQ, int TC, int DP, class F> auto for_heads(int32_t group, F f) {
-    if constexpr (DP <= 64 || (DP == 128 && !(TQ == KV_BF16 && TC == KV_E4M3)))
+    if constexpr (DP <= 128)
         if (group > 8) return f(Dec<TQ, TC, DP, 2>());
     return f(Dec<TQ, TC, DP, 1>());
 }
@@ -1610,6 +1650,7 @@ rt_status kv_decode(const kv_cache* cache, const kv_rows* q, const kv_rows* out,
     A.table = d_page_table; A.len = d_lengths; A.table_stride = table_stride; A.n_seqs = n_seqs;
     A.group = q->n_heads / cache->n_heads; A.max_tokens = max_pages * cache->page_size; A.window = window; A.scale = scale;
     A.lse = d_lse;
+    A.q_words = reinterpret_cast<uintptr_t>(q->data) % 4 == 0 && q->stride[0] % 2 == 0 && q->stride[1] % 2 == 0;
     A.weight = A.max_tokens > 0 ? d_weight : nullptr;
     A.ws[0] = d_weight ? weight_stride[0] : 0; A.ws[1] = d_weight ? weight_stride[1] : 0;
     return for_decode(q->dtype, cache->dtype, cache->head_dim, A.group, [&](auto x) {
