@@ -9,6 +9,8 @@
 #include <stdint.h>
 #include <stdio.h>
 #include <atomic>
+#include <type_traits>
+#include <utility>
 
 #include "klpm_kv.h"
 
@@ -340,38 +342,44 @@ __device__ __forceinline__ long long span_of(long long total, int32_t warps) {
 }
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {      // bytes 0: 16 zeros, nothing is read
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
+template <int OFF> __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {      // bytes 0: 16 zeros, nothing is read
+    asm volatile("cp.async.cg.shared.global [%0 + %3], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes), "n"(OFF) : "memory");
+}
+template <int OFF> __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0 + %2], [%1], 16;" :: "r"(dst), "l"(src), "n"(OFF) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
-__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t a) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+template <int OFF> __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4 + %5];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a), "n"(OFF) : "memory");
 }
-__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t a) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+template <int OFF> __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4 + %5];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a), "n"(OFF) : "memory");
 }
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
+template <int OFF> __device__ __forceinline__ uint4 lds128(uint32_t a) {
     uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4 + %5];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a), "n"(OFF) : "memory");
     return v;
 }
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
+template <int OFF> __device__ __forceinline__ uint2 lds64(uint32_t a) {
     uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2 + %3];" : "=r"(v.x), "=r"(v.y) : "r"(a), "n"(OFF) : "memory");
     return v;
 }
+// f(0), f(1), ... f(N - 1) with constants
+template <class F, int... I> __device__ __forceinline__ void unrolled_(F& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
+template <int N, class F> __device__ __forceinline__ void unrolled(F f) { unrolled_(f, std::make_integer_sequence<int, N>()); }
 template <bool HALF> __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     if constexpr (HALF)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {          // of 16-bit elements, lane 4r + j holding columns 2j, 2j+1 of row r
     uint32_t r;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
 }
 __device__ __forceinline__ uint32_t e4m3_to_f16(uint32_t two) {           // exact; the low 16 bits hold two values
@@ -401,7 +409,9 @@ __device__ __forceinline__ float exp2_fast(float x) {        // 2 ulp; 2^-inf = 
 
 // Where chunk c of row r is, in 16-byte units.  Two-byte types: the eight rows of an ldmatrix lie in eight different 16-byte
 // columns.  8-bit keys: lanes read chunks j, j < 4, of rows 2i and 2i+1 together; 8-bit values: chunks n, n+1 (or half chunks) of rows 0, 2, 4, 6.
-template <class X, bool VALUE> __device__ __forceinline__ int place(int r, int c) {
+// place(a + b, c) = (place(a, c) ^ (place(b, 0) - b rows)) + b rows for a multiple b of a power of two above a: addresses of a lane differ
+// by constants.
+template <class X, bool VALUE> __host__ __device__ constexpr int place(int r, int c) {
     if constexpr (!X::E8) return r * X::CH + (c ^ (r & 7));
     else if constexpr (X::CH == 4) return VALUE ? (r >> 1) * 8 + ((((r & 1) << 2) + c) ^ (((r >> 1) & 3) << 1)) : r * 4 + c;
     else if constexpr (!VALUE) return r * X::CH + (c ^ ((r & 1) << 2));
@@ -421,8 +431,8 @@ template <class X> __device__ __forceinline__ int out_element(int x, int r, int 
     else return x * 16 + r + 8 * e;
 }
 
-template <class X> struct Cursor {       // a tile of the batch
-    int32_t b, u, tile, first, end, lo, hi;
+template <class X> struct Cursor {       // a tile of the batch: of sequence b, unit (cache head g, its query heads from 8 NT ht on)
+    int32_t b, g, ht, tile, first, end, lo, hi;
     __device__ __forceinline__ void row(const DecodeArgs& A) {           // to the first tile of sequence b or of the next one that has any
         for (; b < A.n_seqs; ++b) {
             token_range(A, b, &lo, &hi);
@@ -435,11 +445,14 @@ template <class X> struct Cursor {       // a tile of the batch
     __device__ __forceinline__ void next(const DecodeArgs& A) {
         if (++tile < end) return;
         tile = first;
-        if (++u < A.units) return;
-        u = 0;
+        if (++ht < A.head_tiles) return;
+        ht = 0;
+        if (++g < A.c.n_heads) return;
+        g = 0;
         ++b;
         row(A);
     }
+    __device__ __forceinline__ int32_t head(const DecodeArgs& A) const { return g * A.group + ht * X::HEADS; }       // the first query head
 };
 
 // One warp computes `left` tiles of the batch from ci on.  finish(tile, begun, ended, heads, m, l, o) is called with what a row came to when the
@@ -463,34 +476,30 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
     };
     int32_t page_next = page_of(), page = -1, at = 0, g_now = 0;           // (at: the lane's token's place in its page)
     int slot_in = 0, tile_in = 0;
+    unsigned there_now = 0;                                   // which tokens of the tile that is being loaded are there
     auto copy_rows = [&](auto value) {
         constexpr bool VALUE = decltype(value)::value;
         constexpr int RPI = 32 / X::CH;                       // rows of one instruction
         const int64_t s0 = VALUE ? A.c.vs[0] : A.c.ks[0], s1 = VALUE ? A.c.vs[1] : A.c.ks[1];
         const char* base = (VALUE ? A.c.v : A.c.k) + g_now * (VALUE ? A.c.vs[2] : A.c.ks[2]) + my_ch * 16;
-        const uint32_t to = ring + slot_in * X::TILE;
-        if (A.c.page_shift >= (TT == 32 ? 5 : 4) && __all_sync(FULL_MASK, lane >= TT || page >= 0)) {
+        const uint32_t to = ring + slot_in * X::TILE + place<X, VALUE>(my_row, my_ch) * 16;
+        if (A.c.page_shift >= (TT == 32 ? 5 : 4) && there_now == (TT == 32 ? 0xffffffffu : 0xffffu)) {
             // the whole tile lies in one page
-            const char* p = base + page * s0 + (at - lane + my_row) * s1;          // (page and at - lane are the same in all lanes below TT)
-            if constexpr (TT < 32) p = base + __shfl_sync(FULL_MASK, page, 0) * s0 + (__shfl_sync(FULL_MASK, at, 0) + my_row) * s1;
-            if (my_ch < chunks) {
-#pragma unroll
-                for (int i = 0; i < TT / RPI; ++i) {
-                    cp_async16(to + place<X, VALUE>(i * RPI + my_row, my_ch) * 16, p, 16);
+            const char* p = base + __shfl_sync(FULL_MASK, page, 0) * s0 + (__shfl_sync(FULL_MASK, at, 0) + my_row) * s1;
+            if (my_ch < chunks)
+                unrolled<TT / RPI>([&](auto i) {
+                    constexpr int R = i.value * RPI, F = place<X, VALUE>(R, 0) * 16 - R * X::ROW;
+                    cp_async16<R * X::ROW>(to ^ F, p);
                     p += RPI * s1;
-                }
-            }
+                });
         } else {
             const int64_t mine = page < 0 ? 0 : page * s0 + at * s1;
-            const bool full = __all_sync(FULL_MASK, lane >= TT || page >= 0);
-            const unsigned there = __ballot_sync(FULL_MASK, page >= 0);
-#pragma unroll
-            for (int i = 0; i < TT / RPI; ++i) {
-                const char* p = base + __shfl_sync(FULL_MASK, mine, i * RPI + my_row);
-                int bytes = 16;
-                if (!full) bytes = (there >> (i * RPI + my_row) & 1) << 4;
-                if (my_ch < chunks) cp_async16(to + place<X, VALUE>(i * RPI + my_row, my_ch) * 16, p, bytes);
-            }
+            unrolled<TT / RPI>([&](auto i) {
+                constexpr int R = i.value * RPI, F = place<X, VALUE>(R, 0) * 16 - R * X::ROW;
+                const char* p = base + __shfl_sync(FULL_MASK, mine, R + my_row);
+                const int bytes = (there_now >> (R + my_row) & 1) << 4;
+                if (my_ch < chunks) cp_async16<R * X::ROW>(to ^ F, p, bytes);
+            });
         }
         if (++slot_in == RING) slot_in = 0;
     };
@@ -498,9 +507,9 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
         if (to_load > 0) {
             page = page_next;
             at = (ci.tile * TT + lane) & in_page;
-            g_now = ci.u / A.head_tiles;
-            const unsigned there = __ballot_sync(FULL_MASK, page >= 0);
-            if (lane == 0) s_there[tile_in & 7] = there;
+            g_now = ci.g;
+            there_now = __ballot_sync(FULL_MASK, page >= 0);
+            if (lane == 0) s_there[tile_in & 7] = there_now;
             ++tile_in;
             if (to_load > 1) {
                 ci.next(A);
@@ -520,9 +529,10 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
 
     const int r8 = lane >> 2, j = lane & 3;
     const float log2e = 1.4426950408889634f;
-    // where the lane's rows of an ldmatrix are: chunk c of row r lies at r * ROW + ((c ^ r) & 7 | c & ~7) * 16.  Keys: tokens 0-15, two chunks;
-    // values: tokens 0-7 and 8-15 of two chunks
-    const int kr = lane & 15, kc = lane >> 4, vr = (lane & 7) + ((lane >> 4) << 3), vc = (lane >> 3) & 1;
+    // what the lane reads of a half tile.  Keys: tokens 0-15, two chunks; values: tokens 0-7 and 8-15 of two chunks
+    const int in_keys = X::E8 ? place<X, false>(r8, j) * 16 : place<X, false>(lane & 15, lane >> 4) * 16;
+    const int in_values = !X::E8 ? place<X, true>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1) * 16
+                        : X::CH == 4 ? place<X, true>(2 * j, r8 >> 1) * 16 + (r8 & 1) * 8 : place<X, true>(2 * j, r8 * (X::CH / 8)) * 16;
     uint32_t qb[NT][KS][2];
     float coef[NT][2], m[NT][2], l[NT][2], o[NT][KS][4];
     bool fresh = true, begun_here = false;
@@ -544,9 +554,8 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
         if (fresh) {                                          // a row begins, or the span begins inside one
             fresh = false;
             begun_here = cc.tile == cc.first;
-            const int32_t g = cc.u / A.head_tiles, h0 = (cc.u - g * A.head_tiles) * X::HEADS;
-            heads = min(X::HEADS, A.group - h0);
-            const char* qp = A.q.p + cc.b * A.q.sr + (int64_t)(g * A.group + h0) * A.q.sh;
+            heads = min(X::HEADS, A.group - cc.ht * X::HEADS);
+            const char* qp = A.q.p + cc.b * A.q.sr + (int64_t)cc.head(A) * A.q.sh;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const bool have = n * 8 + r8 < heads;
@@ -606,34 +615,30 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma16816<X::HALF>(s[n][t], a0, a1, a2, a3, qb[n][ks][0], qb[n][ks][1]);
         };
+        const uint32_t key = sk + in_keys;
         if constexpr (X::E8) {
-#pragma unroll
-            for (int hb = 0; hb < X::DP / 64; ++hb) {
-                if (hb * 64 >= A.c.dim) break;
-#pragma unroll
-                for (int t = 0; t < TN; ++t) {
-                    const uint4 a = lds128(sk + place<X, false>(t * 16 + r8, hb * 4 + j) * 16), b = lds128(sk + place<X, false>(t * 16 + 8 + r8, hb * 4 + j) * 16);
+            unrolled<X::DP / 64>([&](auto h) {
+                constexpr int hb = h.value;
+                if (hb * 64 >= A.c.dim) return;
+                unrolled<TN>([&](auto u) {
+                    constexpr int t = u.value, OFF = t * 16 * X::ROW + (hb >> 1) * 128;
+                    const uint4 a = lds128<OFF>(key ^ (hb & 1) * 64), b = lds128<OFF + 8 * X::ROW>(key ^ (hb & 1) * 64);
                     kq(t, hb * 4 + 0, e4m3_to_f16(a.x), e4m3_to_f16(b.x), e4m3_to_f16(a.x >> 16), e4m3_to_f16(b.x >> 16));
                     kq(t, hb * 4 + 1, e4m3_to_f16(a.y), e4m3_to_f16(b.y), e4m3_to_f16(a.y >> 16), e4m3_to_f16(b.y >> 16));
                     kq(t, hb * 4 + 2, e4m3_to_f16(a.z), e4m3_to_f16(b.z), e4m3_to_f16(a.z >> 16), e4m3_to_f16(b.z >> 16));
                     kq(t, hb * 4 + 3, e4m3_to_f16(a.w), e4m3_to_f16(b.w), e4m3_to_f16(a.w >> 16), e4m3_to_f16(b.w >> 16));
-                }
-            }
+                });
+            });
         } else {
-#pragma unroll
-            for (int k4 = 0; k4 < KS; k4 += 4) {
-                if (k4 * 16 >= A.c.dim) break;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t base = sk + kr * X::ROW + (((2 * k + kc) ^ kr) & 7) * 16;
-#pragma unroll
-                    for (int t = 0; t < TN; ++t) {
-                        uint32_t a[4];          // tokens 0-7 and 8-15 of elements 0-7, then of 8-15
-                        ldmatrix4(a, base + t * 16 * X::ROW + k4 * 32);
-                        kq(t, k4 + k, a[0], a[1], a[2], a[3]);
-                    }
-                }
-            }
+            unrolled<KS>([&](auto k) {
+                constexpr int ks = k.value;
+                if (ks / 4 * 64 >= A.c.dim) return;
+                unrolled<TN>([&](auto u) {
+                    uint32_t a[4];              // tokens 0-7 and 8-15 of elements 0-7, then of 8-15
+                    ldmatrix4<u.value * 16 * X::ROW + ks / 4 * 128>(a, key ^ ks % 4 * 32);
+                    kq(u.value, ks, a[0], a[1], a[2], a[3]);
+                });
+            });
         }
         // p = 2^(s - m): tokens r8 and r8 + 8 of heads 2j and 2j + 1
         const unsigned have = s_there[tile_out++ & 7];
@@ -661,8 +666,7 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) grown |= s[n][t][i] > m[n][i & 1];
         if (A.weight) {
-            const int32_t g = cc.u / A.head_tiles, h0 = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS;
-            float* row = A.score + ((int64_t)cc.b * A.q.heads + h0) * A.score_len + (int64_t)cc.tile * TT + r8;
+            float* row = A.score + ((int64_t)cc.b * A.q.heads + cc.head(A)) * A.score_len + (int64_t)cc.tile * TT + r8;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -720,25 +724,23 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
                 mma16816<X::HALF>(o[n][x], a0, a1, a2, a3, pl[n][t][0], pl[n][t][1]);
             }
         };
+        const uint32_t value = sv + in_values;
         if constexpr (X::E8) {
-#pragma unroll
-            for (int t = 0; t < TN; ++t) {
-                constexpr int W = X::DP / 32;                 // words of a lane's elements
+            unrolled<TN>([&](auto u) {
+                constexpr int t = u.value, W = X::DP / 32;    // words of a lane's elements
                 uint32_t v[4][W];                             // tokens 2j, 2j+1, 2j+8, 2j+9
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = t * 16 + 2 * j + (i & 1) + (i >> 1) * 8;
+                unrolled<4>([&](auto k) {
+                    constexpr int i = k.value, OFF = (t * 16 + (i >> 1) * 8 + (X::CH == 4 ? 0 : i & 1)) * X::ROW;
                     if constexpr (X::CH == 4) {
-                        const uint2 a = lds64(sv + place<X, true>(r, r8 >> 1) * 16 + (r8 & 1) * 8);
+                        const uint2 a = lds64<OFF>(value ^ (i & 1) * 64);
                         v[i][0] = a.x; v[i][1] = a.y;
                     } else {
-#pragma unroll
-                        for (int c = 0; c < W / 4; ++c) {
-                            const uint4 a = lds128(sv + place<X, true>(r, r8 * (W / 4) + c) * 16);
-                            v[i][c * 4] = a.x; v[i][c * 4 + 1] = a.y; v[i][c * 4 + 2] = a.z; v[i][c * 4 + 3] = a.w;
-                        }
+                        unrolled<W / 4>([&](auto c) {
+                            const uint4 a = lds128<OFF>(value ^ c.value * 16);
+                            v[i][c.value * 4] = a.x; v[i][c.value * 4 + 1] = a.y; v[i][c.value * 4 + 2] = a.z; v[i][c.value * 4 + 3] = a.w;
+                        });
                     }
-                }
+                });
 #pragma unroll
                 for (int x = 0; x < KS; ++x) {
                     // bytes 2x, 2x+1 of two tokens each: (token 0, token 1) of element 2x, then of 2x+1
@@ -746,22 +748,17 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
                     const uint32_t a = __byte_perm(v[0][x / 2], v[1][x / 2], sel), b = __byte_perm(v[2][x / 2], v[3][x / 2], sel);
                     vp(x, t, e4m3_to_f16(a), e4m3_to_f16(a >> 16), e4m3_to_f16(b), e4m3_to_f16(b >> 16));
                 }
-            }
+            });
         } else {
-#pragma unroll
-            for (int x4 = 0; x4 < KS; x4 += 4) {
-                if (x4 * 16 >= A.c.dim) break;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const uint32_t base = sv + vr * X::ROW + (((2 * x + vc) ^ vr) & 7) * 16;
-#pragma unroll
-                    for (int t = 0; t < TN; ++t) {
-                        uint32_t a[4];          // elements 0-7 and 8-15 of tokens 0-7, then of 8-15
-                        ldmatrix4_trans(a, base + t * 16 * X::ROW + x4 * 32);
-                        vp(x4 + x, t, a[0], a[1], a[2], a[3]);
-                    }
-                }
-            }
+            unrolled<KS>([&](auto k) {
+                constexpr int x = k.value;
+                if (x / 4 * 64 >= A.c.dim) return;
+                unrolled<TN>([&](auto u) {
+                    uint32_t a[4];              // elements 0-7 and 8-15 of tokens 0-7, then of 8-15
+                    ldmatrix4_trans<u.value * 16 * X::ROW + x / 4 * 128>(a, value ^ x % 4 * 32);
+                    vp(x, u.value, a[0], a[1], a[2], a[3]);
+                });
+            });
         }
         // the row ends, or the span
         const bool row_ends = cc.tile + 1 == cc.end;
@@ -1005,11 +1002,12 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
     if (pos >= total) return;
 
     Cursor<X> ci;                                             // the tile that is loaded next
-    ci.b = s_b[warp]; ci.u = 0;
+    ci.b = s_b[warp];
     ci.row(A);
     {
         const long long rem = s_rem[warp];
-        ci.u = (int32_t)(rem / (ci.end - ci.first));
+        const int32_t u = (int32_t)(rem / (ci.end - ci.first));
+        ci.g = u / A.head_tiles; ci.ht = u - ci.g * A.head_tiles;
         ci.tile = ci.first + (int32_t)(rem % (ci.end - ci.first));
     }
     bool first_piece = true;
@@ -1019,7 +1017,7 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
             write_part<X>(A.part + ((int64_t)w * 2 + (first_piece ? 0 : 1)) * X::PART, m, l, o);
         } else {
             const int r8 = lane >> 2, j = lane & 3;
-            const int32_t g = cc.u / A.head_tiles, h0 = g * A.group + (cc.u - g * A.head_tiles) * X::HEADS;
+            const int32_t h0 = cc.head(A);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -1105,14 +1103,14 @@ __global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_k
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int32_t rank = blockIdx.x % ctas, row = blockIdx.x / ctas;
     Cursor<X> c;
-    c.b = row / A.units; c.u = row - c.b * A.units;
+    c.b = row / A.units;
+    c.g = (row - c.b * A.units) / A.head_tiles; c.ht = row - c.b * A.units - c.g * A.head_tiles;
     token_range(A, c.b, &c.lo, &c.hi);
     c.first = c.lo / TT;
     c.end = c.hi > c.lo ? (c.hi + TT - 1) / TT : c.first;
     const int32_t tiles = c.end - c.first, warps = ctas * KLPM_ROW_WARPS, per = (tiles + warps - 1) / warps;
     const int32_t parts = per > 0 ? (tiles + per - 1) / per : 0;
-    const int32_t g = c.u / A.head_tiles, h0 = g * A.group + (c.u - g * A.head_tiles) * X::HEADS;
-    const int32_t heads = min(X::HEADS, A.group - (c.u - g * A.head_tiles) * X::HEADS);
+    const int32_t g = c.g, h0 = c.head(A), heads = min(X::HEADS, A.group - c.ht * X::HEADS);
     clear_ring<X>(A, smem, KLPM_ROW_WARPS * X::WARP_SMEM);
     __syncthreads();
     const int32_t mine = warp * ctas + rank;                  // neighbouring parts on different SMs
@@ -1127,27 +1125,22 @@ __global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_k
         });
     }
     cluster.sync();
-    // output tiles: where parts are few, one per warp of the cluster; else one per CTA at a time, the parts shared by its warps
+    // output tiles: as many of a CTA's warps to each as there are, a part of the parts to every warp
     auto part = [&](int k) { return reinterpret_cast<const float*>(cluster.map_shared_rank(smem, k % ctas) + k / ctas * X::WARP_SMEM); };
-    Joined<X> J;
-    if (parts <= 16) {
-        for (int x = mine; x < KS; x += warps) {
-            J.clear();
-            J.template add<4>(x, 0, 1, parts, part);
-            write_joined<X>(A, J, c.b, h0, heads, x);
-        }
-    } else {
-        for (int x = rank; x < KS; x += ctas) {
-            J.clear();
-            J.template add<4>(x, warp, KLPM_ROW_WARPS, parts, part);
+    const int share = parts <= 4 ? 1 : max(1, min(KLPM_ROW_WARPS, warps / KS)), at = warp / share;          // (powers of two)
+    const int per_cta = KLPM_ROW_WARPS / share;
+    for (int x0 = rank * per_cta; x0 < KS; x0 += ctas * per_cta) {
+        const int x = x0 + at;
+        Joined<X> J;
+        J.clear();
+        if (x < KS) J.template add<4>(x, warp % share, share, parts, part);
+        if (share > 1) {
             J.put(s_all + warp * NT * 2 * 32);
             __syncthreads();
-            if (warp == 0) {
-                J.take(s_all, KLPM_ROW_WARPS);
-                write_joined<X>(A, J, c.b, h0, heads, x);
-            }
-            __syncthreads();
+            if (warp % share == 0) J.take(s_all + warp * NT * 2 * 32, share);
         }
+        if (x < KS && warp % share == 0) write_joined<X>(A, J, c.b, h0, heads, x);
+        if (share > 1) __syncthreads();
     }
     if (A.weight) {                                           // (one unit per cache head)
         for (int hd = warp; hd < heads; hd += KLPM_ROW_WARPS) {
