@@ -509,11 +509,12 @@ def _ints(t: torch.Tensor, cache: KvCache, n: int, name: str) -> int:
 
 def _pages(t: torch.Tensor, cache: KvCache, n: int, name: str):
     """Pointer, row stride and width of a page table."""
-    shape = t.shape
-    if len(shape) != 2 or shape[0] != n or t.device != cache.device:
-        raise ValueError("%s must have one row per sequence, on the cache's device" % name)
-    p, stride = _table(t, name)
-    return p, stride, shape[1]
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not torch.int32 or len(shape) != 2 or shape[0] != n or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError("%s must be an int32 tensor with one contiguous row per sequence" % name)
+    if t.device != cache.device:
+        raise ValueError("%s must be on the cache's device" % name)
+    return t.data_ptr(), stride[0], shape[1]
 
 
 def kv_rope_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None,

@@ -302,8 +302,6 @@ struct DecodeArgs {
 #define KLPM_DECODE_WARPS 4             // of a CTA
 #define KLPM_DECODE_MIN_SPAN 2          // tiles
 #define KLPM_SMS 148
-#define KLPM_ROW_TOKENS 16384            // the most a sequence may have, and tiles per warp of the GPU, for decode_row_kernel
-#define KLPM_ROW_TILES 8
 
 template <int TQ_, int TC_, int DP_, int NT_> struct Dec {
     static constexpr int TQ = TQ_, TC = TC_, DP = DP_, NT = NT_;
@@ -488,17 +486,17 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
             const char* p = base + __shfl_sync(FULL_MASK, page, 0) * s0 + (__shfl_sync(FULL_MASK, at, 0) + my_row) * s1;
             if (my_ch < chunks)
                 unrolled<TT / RPI>([&](auto i) {
-                    constexpr int R = i.value * RPI, F = place<X, VALUE>(R, 0) * 16 - R * X::ROW;
-                    cp_async16<R * X::ROW>(to ^ F, p);
+                    constexpr int R = i.value * RPI, FLIP = place<X, VALUE>(R, 0) * 16 - R * X::ROW;
+                    cp_async16<R * X::ROW>(to ^ FLIP, p);
                     p += RPI * s1;
                 });
         } else {
             const int64_t mine = page < 0 ? 0 : page * s0 + at * s1;
             unrolled<TT / RPI>([&](auto i) {
-                constexpr int R = i.value * RPI, F = place<X, VALUE>(R, 0) * 16 - R * X::ROW;
+                constexpr int R = i.value * RPI, FLIP = place<X, VALUE>(R, 0) * 16 - R * X::ROW;
                 const char* p = base + __shfl_sync(FULL_MASK, mine, R + my_row);
                 const int bytes = (there_now >> (R + my_row) & 1) << 4;
-                if (my_ch < chunks) cp_async16<R * X::ROW>(to ^ F, p, bytes);
+                if (my_ch < chunks) cp_async16<R * X::ROW>(to ^ FLIP, p, bytes);
             });
         }
         if (++slot_in == RING) slot_in = 0;
@@ -606,14 +604,16 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
         const uint32_t sk = step();
         if constexpr (RING & 1) load_keys();
         else load_values();
-        float s[NT][TN][4];
+        float s[NT][TN][4], s2[NT][TN][4];                    // (sums of every other step: shorter chains)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int t = 0; t < TN; ++t) s[n][t][0] = s[n][t][1] = s[n][t][2] = s[n][t][3] = 0.0f;
+            for (int t = 0; t < TN; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[n][t][i] = s2[n][t][i] = 0.0f;
         auto kq = [&](int t, int ks, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma16816<X::HALF>(s[n][t], a0, a1, a2, a3, qb[n][ks][0], qb[n][ks][1]);
+            for (int n = 0; n < NT; ++n) mma16816<X::HALF>(ks & 1 ? s2[n][t] : s[n][t], a0, a1, a2, a3, qb[n][ks][0], qb[n][ks][1]);
         };
         const uint32_t key = sk + in_keys;
         if constexpr (X::E8) {
@@ -648,7 +648,7 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
 #pragma unroll
             for (int t = 0; t < TN; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[n][t][i] *= coef[n][i & 1];
+                for (int i = 0; i < 4; ++i) s[n][t][i] = (s[n][t][i] + s2[n][t][i]) * coef[n][i & 1];
         if (have != (TT == 32 ? 0xffffffffu : 0xffffu)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -717,12 +717,16 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
         const uint32_t sv = step();
         if constexpr (RING & 1) load_values();
         else load_keys();
-        auto vp = [&](int x, int t, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+        auto vp = [&](int x, int t, const uint32_t (&a)[2][4]) {         // output tiles x, x + 1: the two products of one sum apart from one another
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                mma16816<X::HALF>(o[n][x], a0, a1, a2, a3, ph[n][t][0], ph[n][t][1]);
-                mma16816<X::HALF>(o[n][x], a0, a1, a2, a3, pl[n][t][0], pl[n][t][1]);
-            }
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint32_t (&p)[2] = half ? pl[n][t] : ph[n][t];
+                        mma16816<X::HALF>(o[n][x + y], a[y][0], a[y][1], a[y][2], a[y][3], p[0], p[1]);
+                    }
         };
         const uint32_t value = sv + in_values;
         if constexpr (X::E8) {
@@ -742,21 +746,27 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
                     }
                 });
 #pragma unroll
-                for (int x = 0; x < KS; ++x) {
+                for (int x = 0; x < KS; x += 2) {
                     // bytes 2x, 2x+1 of two tokens each: (token 0, token 1) of element 2x, then of 2x+1
-                    const uint32_t sel = x & 1 ? 0x7362 : 0x5140;
-                    const uint32_t a = __byte_perm(v[0][x / 2], v[1][x / 2], sel), b = __byte_perm(v[2][x / 2], v[3][x / 2], sel);
-                    vp(x, t, e4m3_to_f16(a), e4m3_to_f16(a >> 16), e4m3_to_f16(b), e4m3_to_f16(b >> 16));
+                    uint32_t a[2][4];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint32_t sel = y ? 0x7362 : 0x5140;
+                        const uint32_t c = __byte_perm(v[0][x / 2], v[1][x / 2], sel), d = __byte_perm(v[2][x / 2], v[3][x / 2], sel);
+                        a[y][0] = e4m3_to_f16(c); a[y][1] = e4m3_to_f16(c >> 16); a[y][2] = e4m3_to_f16(d); a[y][3] = e4m3_to_f16(d >> 16);
+                    }
+                    vp(x, t, a);
                 }
             });
         } else {
-            unrolled<KS>([&](auto k) {
-                constexpr int x = k.value;
+            unrolled<KS / 2>([&](auto k) {
+                constexpr int x = k.value * 2;
                 if (x / 4 * 64 >= A.c.dim) return;
                 unrolled<TN>([&](auto u) {
-                    uint32_t a[4];              // elements 0-7 and 8-15 of tokens 0-7, then of 8-15
-                    ldmatrix4_trans<u.value * 16 * X::ROW + x / 4 * 128>(a, value ^ x % 4 * 32);
-                    vp(x, u.value, a[0], a[1], a[2], a[3]);
+                    uint32_t a[2][4];           // elements 0-7 and 8-15 of tokens 0-7, then of 8-15
+                    ldmatrix4_trans<u.value * 16 * X::ROW + x / 4 * 128>(a[0], value ^ x % 4 * 32);
+                    ldmatrix4_trans<u.value * 16 * X::ROW + x / 4 * 128>(a[1], value ^ (x % 4 + 1) * 32);
+                    vp(x, u.value, a);
                 });
             });
         }
@@ -1046,16 +1056,16 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
     });
 }
 
-// Rows that were cut into parts, and rows with nothing to attend to.  An item is 16 elements of a unit.  WPR = 8: a CTA per item, where few
-// rows have many parts each.  WPR = 1: a warp per item, where many rows have few.
+// Rows that were cut into parts, and rows with nothing to attend to.  An item is 16 elements of a unit, for WPR warps: a CTA where few rows
+// have many parts each, a warp where many rows have few.
 template <class X, int WPR>
-__global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant__ DecodeArgs A) {
+__global__ void __launch_bounds__(WPR == 1 ? 256 : WPR * 32) decode_join_kernel(const __grid_constant__ DecodeArgs A) {
     using Q = typename Elem<X::TQ>::T;
-    __shared__ float4 s_all[WPR == 8 ? 8 * X::NT * 2 * 32 : 1];
+    __shared__ float4 s_all[WPR > 1 ? WPR * X::NT * 2 * 32 : 1];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t item = WPR == 8 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + warp, row = item / X::KS;
+    const int64_t item = WPR > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + warp, row = item / X::KS;
     const int x = (int)(item % X::KS);
     if (row >= (int64_t)A.n_seqs * A.units) return;
     const int32_t b = (int32_t)(row / A.units), u = (int32_t)(row % A.units), g = u / A.head_tiles, in = (u - g * A.head_tiles) * X::HEADS;
@@ -1065,7 +1075,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
     const long long R = t0 * A.units + u * tiles, E = R + tiles;
     const int32_t w0 = (int32_t)(R / span), parts = tiles > 0 ? (int32_t)((E - 1) / span) - w0 + 1 : 0;
     if (parts == 1) {                                        // decode_kernel has written it; is there anything to repair?
-        if (WPR == 8 && warp) return;
+        if (WPR > 1 && warp) return;
         const int d = out_element<X>(x, lane & 7, (lane >> 3) & 1);
         for (int32_t hd = 0; hd < heads; ++hd) {
             const Q* out = reinterpret_cast<const Q*>(A.out.p + b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
@@ -1077,12 +1087,12 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
     const int first = w0 * span == R ? 0 : 1;
     Joined<X> J;
     J.clear();
-    J.template add<4>(x, WPR == 8 ? warp : 0, WPR, parts, [&](int k) { return A.part + ((int64_t)(w0 + k) * 2 + (k == 0 ? first : 0)) * X::PART; });
-    if constexpr (WPR == 8) {
+    J.template add<4>(x, WPR > 1 ? warp : 0, WPR, parts, [&](int k) { return A.part + ((int64_t)(w0 + k) * 2 + (k == 0 ? first : 0)) * X::PART; });
+    if constexpr (WPR > 1) {
         J.put(s_all + warp * X::NT * 2 * 32);
         __syncthreads();
         if (warp) return;
-        J.take(s_all, 8);
+        J.take(s_all, WPR);
     }
     write_joined<X>(A, J, b, h0, heads, x);
 }
@@ -1090,6 +1100,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
 // Small calls: a cluster of CTAs per row (sequence, unit), its tiles dealt out to all of the cluster's warps, whose results are joined through
 // distributed shared memory: one kernel, no trip through the workspace.  Weights are added from the scores by the warps that made them.
 #define KLPM_ROW_WARPS 8
+#define KLPM_ROW_CTAS 16
 template <class X>
 __global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_kernel(const __grid_constant__ DecodeArgs A, int32_t ctas) {
     using Q = typename Elem<X::TQ>::T;
@@ -1251,6 +1262,7 @@ template <auto kernel> rt_status allow_smem(int bytes) {
     const uint64_t bit = 1ull << (dev & 63);
     if (asked.load(std::memory_order_relaxed) & bit) return RT_OK;
     CK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    CK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     asked.fetch_or(bit, std::memory_order_relaxed);
     return RT_OK;
 }
@@ -1283,11 +1295,17 @@ template <class X> rt_status launch_decode(DecodeArgs& A, char* work, cudaStream
     const DecodeSpace W = decode_space(A.n_seqs, A.q.heads, A.max_tokens, A.warps, X::PART, A.weight != nullptr);
     A.tiles_before = (long long*)work; A.lse2 = (float*)(work + W.lse2); A.part = (float*)(work + W.part); A.score = (float*)(work + W.score);
     A.score_len = W.score_len;
-    const long long tiles = (A.max_tokens + X::TT - 1) / X::TT, units = (long long)A.n_seqs * A.units;
-    if (A.max_tokens <= KLPM_ROW_TOKENS && units * (tiles ? tiles : 1) <= (long long)KLPM_ROW_TILES * A.warps && (!A.weight || A.head_tiles == 1)) {
-        // CTAs of a cluster: until every warp has a tile or the GPU is full
-        int ctas = 1;
-        while (ctas < 8 && ctas * KLPM_ROW_WARPS < tiles && units * ctas * 2 <= KLPM_SMS * (X::CTAS / 2)) ctas *= 2;
+    // the most tiles of a row: a window that begins inside a tile takes one more
+    const long long seen = A.window > 0 && A.window < A.max_tokens ? (long long)A.window + X::TT : A.max_tokens;
+    const long long tiles = seen / X::TT + 1, units = (long long)A.n_seqs * A.units;
+    // CTAs of a cluster: until every warp has a tile or the GPU is full (by half with clusters of 8, by a quarter with 16, which have to
+    // find their SMs in one GPC: 16 clusters of 16 take 16.6 us where as many of 8 take 10.3)
+    int ctas = 1;
+    while (ctas < KLPM_ROW_CTAS && ctas * KLPM_ROW_WARPS < tiles
+           && units * ctas * 2 <= KLPM_SMS * (X::CTAS / 2) / (ctas < 4 ? 1 : ctas / 2)) ctas *= 2;
+    // The other kernels start 4.5 us later, but deal out the tiles evenly; a tile per warp takes 1.2 us while the GPU is not full.
+    // (128 units: of 65 tiles 22.8 us here, 25.0 us there; of 129 tiles of half the bytes 22.9 us, 19.3 us)
+    if (units * tiles <= 4LL * A.warps && tiles <= (long long)ctas * KLPM_ROW_WARPS * (4 + units * tiles / A.warps) && (!A.weight || A.head_tiles == 1)) {
         constexpr int bytes = KLPM_ROW_WARPS * X::WARP_SMEM;
         if (rt_status st = allow_smem<decode_row_kernel<X>>(bytes)) return st;
         return launch_cluster(decode_row_kernel<X>, (unsigned)(units * ctas), KLPM_ROW_WARPS * 32, ctas, bytes, s, A, (int32_t)ctas);
@@ -1295,11 +1313,13 @@ template <class X> rt_status launch_decode(DecodeArgs& A, char* work, cudaStream
     if (rt_status st = allow_smem<decode_kernel<X>>(X::SMEM)) return st;
     decode_kernel<X><<<KLPM_SMS * X::CTAS, KLPM_DECODE_WARPS * 32, X::SMEM, s>>>(A);
     CK(cudaGetLastError());
-    // a unit has A.warps / units parts or so: with more than a few of them, eight warps share them
+    // a unit has A.warps / units parts or so
     const int64_t items = units * X::KS;
     if (items > 0x7fffffffLL) return RT_ERR_TOO_LARGE;
-    rt_status st = units * 4 <= A.warps ? launch_after(decode_join_kernel<X, 8>, dim3((unsigned)items), 256, s, A)
-                                        : launch_after(decode_join_kernel<X, 1>, dim3((unsigned)((items + 7) / 8)), 256, s, A);
+    constexpr int MANY = 32 / X::NT;
+    rt_status st = units * 64 <= A.warps   ? launch_after(decode_join_kernel<X, MANY>, dim3((unsigned)items), MANY * 32, s, A)
+                   : units * 16 <= A.warps ? launch_after(decode_join_kernel<X, 8>, dim3((unsigned)items), 256, s, A)
+                                           : launch_after(decode_join_kernel<X, 1>, dim3((unsigned)((items + 7) / 8)), 256, s, A);
     if (st || !A.weight) return st;
     return launch_after(decode_weight_kernel<X::TT>, dim3(KLPM_SMS * 4), 256, s, A);
 }
@@ -1338,52 +1358,111 @@ struct EvictArgs {
 
 // What a token is ranked by, larger first: 0 = not there, then NaN, the numbers in their order, and what is kept in any case.
 __device__ __forceinline__ unsigned evict_key(const EvictArgs& A, int32_t b, int32_t g, int32_t n, int32_t t) {
-    if (t >= n) return 0u;
-    const int32_t page = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
-    if ((unsigned)page >= (unsigned)A.c.n_pages) return 0u;
-    if (t < A.sinks || t >= n - A.recent) return 0xffffffffu;
     const float w = __ldg(A.weight + b * A.ws[0] + g * A.ws[1] + t);
-    if (w != w) return 1u;
+    const int32_t page = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
     const unsigned u = __float_as_uint(w == 0.0f ? 0.0f : w);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    unsigned k = u & 0x80000000u ? ~u : u | 0x80000000u;
+    if (w != w) k = 1u;
+    if (t < A.sinks || t >= n - A.recent) k = 0xffffffffu;
+    return (unsigned)page < (unsigned)A.c.n_pages ? k : 0u;
+}
+
+// Copies `rows` kept rows of cache head g, keys and values: lane r holds where row r is (sk, sv) and goes (dk, dv; byte offsets, sk < 0: nothing
+// to copy).  16 bytes a lane, eight loads in flight.
+__device__ __forceinline__ void copy_kept(const EvictArgs& A, int rows, int64_t sk, int64_t sv, int64_t dk, int64_t dv) {
+    const int lane = threadIdx.x & 31;
+    const unsigned slots = A.row_bytes / 8;        // 16-byte pieces of a row's key and value together, at most 64
+    const unsigned magic = (1u << 20) / slots + 1; // e * magic >> 20 = e / slots for e < 2^20 / slots
+    constexpr int DEEP = 8;
+    for (unsigned e0 = 0; e0 < rows * slots; e0 += 32 * DEEP) {
+        int4 v[DEEP];
+        char* to[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            const unsigned e = e0 + i * 32 + lane;
+            const unsigned r = e * magic >> 20, x = e - r * slots;
+            const int64_t s0 = __shfl_sync(FULL_MASK, sk, r & 31), s1 = __shfl_sync(FULL_MASK, sv, r & 31);
+            const int64_t d0 = __shfl_sync(FULL_MASK, dk, r & 31), d1 = __shfl_sync(FULL_MASK, dv, r & 31);
+            const bool value = x >= slots / 2;
+            to[i] = nullptr;
+            if (r < rows && s0 >= 0) {
+                to[i] = value ? A.c.v + d1 + (x - slots / 2) * 16 : A.c.k + d0 + x * 16;
+                v[i] = *reinterpret_cast<const int4*>(value ? A.c.v + s1 + (x - slots / 2) * 16 : A.c.k + s0 + x * 16);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+            if (to[i]) *reinterpret_cast<int4*>(to[i]) = v[i];
+    }
+}
+// Where token t of sequence b is, and its place j in the new pages.
+__device__ __forceinline__ void kept_row(const EvictArgs& A, int32_t b, int32_t g, int32_t t, int64_t j, int64_t* sk, int64_t* sv, int64_t* dk, int64_t* dv) {
+    const int32_t in_page = (1 << A.c.page_shift) - 1;
+    const int32_t from = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
+    const int32_t to = __ldg(A.new_table + b * A.new_stride + (j >> A.c.page_shift));
+    if ((unsigned)from >= (unsigned)A.c.n_pages || (unsigned)to >= (unsigned)A.c.n_pages) return;
+    *sk = from * A.c.ks[0] + (t & in_page) * A.c.ks[1] + g * A.c.ks[2];
+    *sv = from * A.c.vs[0] + (t & in_page) * A.c.vs[1] + g * A.c.vs[2];
+    *dk = to * A.c.ks[0] + (j & in_page) * A.c.ks[1] + g * A.c.ks[2];
+    *dv = to * A.c.vs[0] + (j & in_page) * A.c.vs[1] + g * A.c.vs[2];
 }
 
 // The kept tokens of a row (sequence, cache head), in order of position.  The key of the last one is found 11, 11 and 10 bits at a
 // time from histograms; then everybody counts what lies before its part.  A row belongs to a cluster of CTAs that see each other's
 // histograms through distributed shared memory, a contiguous part each, so that few long rows use many SMs.  HELD: the keys of a CTA's
-// part stay in shared memory (4 bytes a token); beyond that they are made again from the weights for each pass.
+// part stay in shared memory (4 bytes a token); beyond that they are made again from the weights for each pass.  COPY: it copies the rows too.
 #define KLPM_EVICT_BINS 2048
 #define KLPM_EVICT_HELD 49152          // keys a CTA holds (192 KB)
 struct EvictShared {
-    int32_t hist[3][KLPM_EVICT_BINS];
+    alignas(16) int32_t hist[3][KLPM_EVICT_BINS];
     int32_t warp_sum[32], warp_eq[32];
     int32_t bin, above, count, total;
     int32_t gt, eq;
 };
 
-template <int T, bool HELD>
+template <int T, bool HELD, bool COPY>
 __global__ void __launch_bounds__(T) evict_select_kernel(const EvictArgs A, int32_t ctas) {
     constexpr int WARPS = T / 32, PER = KLPM_EVICT_BINS / T;
     extern __shared__ __align__(16) unsigned s_key[];
     __shared__ EvictShared S;
+    __shared__ int s_lane[COPY ? WARPS : 1][32];
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int32_t rank = blockIdx.x % ctas, row = blockIdx.x / ctas;
     const int32_t b = row / A.c.n_heads, g = row % A.c.n_heads;
     int32_t n = __ldg(A.len + b);
+    for (int i = tid; i < 3 * KLPM_EVICT_BINS / 4; i += T) reinterpret_cast<int4*>(&S.hist[0][0])[i] = make_int4(0, 0, 0, 0);
     n = n < 0 ? 0 : n > A.max_tokens ? A.max_tokens : n;
     const int32_t part = ((n + ctas - 1) / ctas + 31) & ~31;
     const int32_t t0 = min((long long)rank * part, (long long)n), t1 = min(t0 + part, n);
     int32_t* index = A.index + (int64_t)row * A.keep;
     const float* w = A.weight + b * A.ws[0] + g * A.ws[1];
     float* nw = A.new_weight + b * A.nws[0] + g * A.nws[1];
-    for (int i = tid; i < 3 * KLPM_EVICT_BINS; i += T) (&S.hist[0][0])[i] = 0;
+    if (ctas > 1) cluster.barrier_arrive();
     __syncthreads();
-    for (int32_t t = t0 + tid; t < t1; t += T) {
-        const unsigned k = evict_key(A, b, g, n, t);
-        if (HELD) s_key[t - t0] = k;
-        if (k) atomicAdd(&S.hist[0][k >> 21], 1);
+    EvictShared* first = cluster.map_shared_rank(&S, 0);
+    // keys, eight of a thread in flight, and the first histogram.  What many tokens have in common -- kept in any case, never looked
+    // at -- is counted per warp: 32 additions to one word of shared memory would take turns
+    constexpr int DEEP = 8;
+    for (int32_t base = t0; base < t1; base += T * DEEP) {
+        unsigned k[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            const int32_t t = base + i * T + tid;
+            k[i] = t < t1 ? evict_key(A, b, g, n, t) : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            const int32_t t = base + i * T + tid;
+            if (HELD && t < t1) s_key[t - t0] = k[i];
+            const int held = __popc(__ballot_sync(FULL_MASK, k[i] == 0xffffffffu)), none = __popc(__ballot_sync(FULL_MASK, k[i] == 0x80000000u));
+            if (lane == 0) {
+                if (held) atomicAdd(&S.hist[0][KLPM_EVICT_BINS - 1], held);
+                if (none) atomicAdd(&S.hist[0][0x80000000u >> 21], none);
+            }
+            if (k[i] && k[i] != 0xffffffffu && k[i] != 0x80000000u) atomicAdd(&S.hist[0][k[i] >> 21], 1);
+        }
     }
     auto key = [&](int32_t t) -> unsigned { return t >= t1 ? 0u : HELD ? s_key[t - t0] : evict_key(A, b, g, n, t); };
     unsigned limit = 0;                        // kept: keys above it, and the first `want` that equal it
@@ -1398,46 +1477,57 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const EvictArgs A, int3
                 if (k && (k >> up) == (limit >> up)) atomicAdd(&S.hist[pass][(k >> shift) & (pass == 1 ? 2047 : 1023)], 1);
             }
         }
-        cluster.sync();
-        // bins from the top: thread 0 has the highest
-        int32_t c[PER], mine = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int bin = KLPM_EVICT_BINS - 1 - (tid * PER + i);
-            int32_t v = 0;
-            for (int r = 0; r < ctas; ++r) v += cluster.map_shared_rank(&S.hist[pass][0], r)[bin];
-            c[i] = v;
-            mine += v;
-        }
-        int32_t upto = mine;
-        for (int d = 1; d < 32; d <<= 1) {
-            const int32_t v = __shfl_up_sync(FULL_MASK, upto, d);
-            if (lane >= d) upto += v;
-        }
-        if (lane == 31) S.warp_sum[warp] = upto;
         __syncthreads();
-        int32_t total = 0;
-        for (int i = 0; i < WARPS; ++i) {
-            if (i < warp) upto += S.warp_sum[i];
-            total += S.warp_sum[i];
+        if (ctas > 1) {
+            if (pass == 0) cluster.barrier_wait();            // the first CTA's histograms are 0 by now
+            if (rank) {
+                for (int i = tid; i < KLPM_EVICT_BINS; i += T) {
+                    const int32_t v = S.hist[pass][i];
+                    if (v) atomicAdd(&first->hist[pass][i], v);
+                }
+            }
+            cluster.sync();
         }
+        if (rank == 0) {
+            // bins from the top: thread 0 has the highest
+            int32_t c[PER], mine = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                c[i] = S.hist[pass][KLPM_EVICT_BINS - 1 - (tid * PER + i)];
+                mine += c[i];
+            }
+            int32_t upto = mine;
+            for (int d = 1; d < 32; d <<= 1) {
+                const int32_t v = __shfl_up_sync(FULL_MASK, upto, d);
+                if (lane >= d) upto += v;
+            }
+            if (lane == 31) S.warp_sum[warp] = upto;
+            __syncthreads();
+            const int32_t sums = lane < WARPS ? S.warp_sum[lane] : 0;
+            upto += __reduce_add_sync(FULL_MASK, lane < warp ? sums : 0);
+            const int32_t total = __reduce_add_sync(FULL_MASK, sums), wanted = pass ? want : min(A.keep, total);
+            int32_t above = upto - mine;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                if (above < wanted && wanted <= above + c[i]) { S.bin = KLPM_EVICT_BINS - 1 - (tid * PER + i); S.above = above; S.count = c[i]; }
+                above += c[i];
+            }
+            if (tid == 0) S.total = total;
+        }
+        if (ctas > 1) cluster.sync();
+        else __syncthreads();
+        const int32_t bin = first->bin, above = first->above, count = first->count;
         if (pass == 0) {
+            const int32_t total = first->total;
             K = min(A.keep, total);
             want = K;
-            if (K == total) { want = 0; break; }            // everything that is there is kept: keys above 0
+            if (K == total) { want = 0; break; }              // everything that is there is kept: keys above 0
         }
-        int32_t above = upto - mine;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if (above < want && want <= above + c[i]) { S.bin = KLPM_EVICT_BINS - 1 - (tid * PER + i); S.above = above; S.count = c[i]; }
-            above += c[i];
-        }
-        __syncthreads();
-        limit |= (unsigned)S.bin << shift;
-        want -= S.above;
-        const bool all = S.count == want;
-        __syncthreads();
-        if (all) { limit = limit ? limit - 1 : 0u; want = 0; break; }      // the whole bin is kept
+        limit |= (unsigned)bin << shift;
+        want -= above;
+        if (count == want) { limit = limit ? limit - 1 : 0u; want = 0; break; }      // the whole bin is kept
+        if (ctas > 1) cluster.sync();                         // (the first CTA writes bin again)
+        else __syncthreads();
     }
     // what lies before: in the warps and the CTAs with earlier tokens
     const int32_t per_warp = (part / 32 + WARPS - 1) / WARPS * 32;
@@ -1452,26 +1542,40 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const EvictArgs A, int3
     __syncthreads();
     if (lane == 0) { S.warp_sum[warp] = gts; S.warp_eq[warp] = eqs; }
     __syncthreads();
-    gts = eqs = 0;
-    int32_t all_gt = 0, all_eq = 0;
-    for (int i = 0; i < WARPS; ++i) {
-        if (i < warp) { gts += S.warp_sum[i]; eqs += S.warp_eq[i]; }
-        all_gt += S.warp_sum[i]; all_eq += S.warp_eq[i];
-    }
+    const int32_t a = lane < WARPS ? S.warp_sum[lane] : 0, e0 = lane < WARPS ? S.warp_eq[lane] : 0;
+    const int32_t all_gt = __reduce_add_sync(FULL_MASK, a), all_eq = __reduce_add_sync(FULL_MASK, e0);
+    gts = __reduce_add_sync(FULL_MASK, lane < warp ? a : 0);
+    eqs = __reduce_add_sync(FULL_MASK, lane < warp ? e0 : 0);
     if (tid == 0) { S.gt = all_gt; S.eq = all_eq; }
-    cluster.sync();
-    for (int r = 0; r < rank; ++r) { gts += *cluster.map_shared_rank(&S.gt, r); eqs += *cluster.map_shared_rank(&S.eq, r); }
-    cluster.sync();                             // nobody leaves while its shared memory is read
+    if (ctas > 1) {
+        cluster.sync();
+        for (int r = 0; r < rank; ++r) { gts += *cluster.map_shared_rank(&S.gt, r); eqs += *cluster.map_shared_rank(&S.eq, r); }
+        cluster.barrier_arrive();               // nobody leaves while its shared memory is read
+    }
     if (K > 0)
         for (int32_t t = a0; t < a1; t += 32) {
             const unsigned k = t + lane < a1 ? key(t + lane) : 0u;
             const bool gt = k > limit, eq = k == limit && k;
             const unsigned bg = __ballot_sync(FULL_MASK, gt), be = __ballot_sync(FULL_MASK, eq), below = (1u << lane) - 1;
-            const int32_t e = eqs + __popc(be & below);
-            if (gt || (eq && e < want)) {
-                const int32_t j = gts + __popc(bg & below) + min(e, want);
+            const int32_t e = eqs + __popc(be & below), j = gts + __popc(bg & below) + min(e, want);
+            const bool kept = gt || (eq && e < want);
+            if (kept) {
                 index[j] = t + lane;
                 nw[j] = __ldg(w + t + lane);
+            }
+            if constexpr (COPY) {
+                const unsigned bk = __ballot_sync(FULL_MASK, kept);
+                int64_t sk = -1, sv = 0, dk = 0, dv = 0;
+                if (kept) {
+                    kept_row(A, b, g, t + lane, j, &sk, &sv, &dk, &dv);
+                    s_lane[warp][__popc(bk & below)] = lane;
+                }
+                __syncwarp();
+                const int from = lane < __popc(bk) ? s_lane[warp][lane] : 0;         // the kept ones side by side
+                __syncwarp();
+                sk = __shfl_sync(FULL_MASK, sk, from); sv = __shfl_sync(FULL_MASK, sv, from);
+                dk = __shfl_sync(FULL_MASK, dk, from); dv = __shfl_sync(FULL_MASK, dv, from);
+                copy_kept(A, __popc(bk), sk, sv, dk, dv);
             }
             gts += __popc(bg);
             eqs += __popc(be);
@@ -1479,6 +1583,7 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const EvictArgs A, int3
     for (int32_t j = K + rank * T + tid; j < A.keep; j += ctas * T) index[j] = -1;
     for (int32_t j = K + rank * T + tid; j < A.new_len; j += ctas * T) nw[j] = 0.0f;
     if (g == 0 && rank == 0 && tid == 0) A.new_lengths[b] = K;
+    if (ctas > 1) cluster.barrier_wait();
 }
 
 // The kept rows, keys and values: a warp looks up ROWS of them, one per lane, then copies them 16 bytes a lane, eight loads in flight.
@@ -1491,49 +1596,17 @@ __global__ void __launch_bounds__(256) evict_copy_kernel(const EvictArgs A) {
     const int64_t j0 = id / A.c.n_heads * ROWS;
     if (j0 >= A.keep) return;
     const int64_t j = j0 + lane;
-    const int32_t in_page = (1 << A.c.page_shift) - 1;
-    int64_t sk = -1, dk = 0, sv = 0, dv = 0;      // sk < 0: nothing to copy
+    int64_t sk = -1, sv = 0, dk = 0, dv = 0;
     if (lane < ROWS && j < A.keep) {
         const int32_t t = A.index[((int64_t)b * A.c.n_heads + g) * A.keep + j];
-        if (t >= 0) {
-            const int32_t from = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
-            const int32_t to = __ldg(A.new_table + b * A.new_stride + (j >> A.c.page_shift));
-            if ((unsigned)from < (unsigned)A.c.n_pages && (unsigned)to < (unsigned)A.c.n_pages) {
-                sk = from * A.c.ks[0] + (t & in_page) * A.c.ks[1] + g * A.c.ks[2];
-                sv = from * A.c.vs[0] + (t & in_page) * A.c.vs[1] + g * A.c.vs[2];
-                dk = to * A.c.ks[0] + (j & in_page) * A.c.ks[1] + g * A.c.ks[2];
-                dv = to * A.c.vs[0] + (j & in_page) * A.c.vs[1] + g * A.c.vs[2];
-            }
-        }
+        if (t >= 0) kept_row(A, b, g, t, j, &sk, &sv, &dk, &dv);
     }
-    const unsigned slots = A.row_bytes / 8;        // 16-byte pieces of a row's key and value together, at most 64
-    const unsigned magic = (1u << 20) / slots + 1; // e * magic >> 20 = e / slots for e < 2^20 / slots
-    constexpr int DEEP = 8;
-    for (unsigned e0 = 0; e0 < ROWS * slots; e0 += 32 * DEEP) {
-        int4 v[DEEP];
-        char* to[DEEP];
-#pragma unroll
-        for (int i = 0; i < DEEP; ++i) {
-            const unsigned e = e0 + i * 32 + lane;
-            const unsigned r = e * magic >> 20, x = e - r * slots;
-            const int64_t s0 = __shfl_sync(FULL_MASK, sk, r & 31), s1 = __shfl_sync(FULL_MASK, sv, r & 31);
-            const int64_t d0 = __shfl_sync(FULL_MASK, dk, r & 31), d1 = __shfl_sync(FULL_MASK, dv, r & 31);
-            const bool value = x >= slots / 2;
-            to[i] = nullptr;
-            if (r < ROWS && s0 >= 0) {
-                to[i] = value ? A.c.v + d1 + (x - slots / 2) * 16 : A.c.k + d0 + x * 16;
-                v[i] = *reinterpret_cast<const int4*>(value ? A.c.v + s1 + (x - slots / 2) * 16 : A.c.k + s0 + x * 16);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < DEEP; ++i)
-            if (to[i]) *reinterpret_cast<int4*>(to[i]) = v[i];
-    }
+    copy_kept(A, ROWS, sk, sv, dk, dv);
 }
 
-template <int T, bool HELD> rt_status launch_select(const EvictArgs& A, int64_t rows, int ctas, size_t smem, cudaStream_t s) {
-    if (rt_status st = allow_smem<evict_select_kernel<T, HELD>>(KLPM_EVICT_HELD * 4)) return st;
-    return launch_cluster(evict_select_kernel<T, HELD>, (unsigned)(rows * ctas), T, ctas, smem, s, A, (int32_t)ctas);
+template <int T, bool HELD, bool COPY> rt_status launch_select(const EvictArgs& A, int64_t rows, int ctas, size_t smem, cudaStream_t s) {
+    if (rt_status st = allow_smem<evict_select_kernel<T, HELD, COPY>>(KLPM_EVICT_HELD * 4)) return st;
+    return launch_cluster(evict_select_kernel<T, HELD, COPY>, (unsigned)(rows * ctas), T, ctas, smem, s, A, (int32_t)ctas);
 }
 
 }  // namespace
@@ -1677,17 +1750,23 @@ rt_status kv_evict(const kv_cache* cache, const float* d_weight, const int64_t* 
     A.new_lengths = d_new_lengths;
     cudaStream_t s = (cudaStream_t)stream;
     const int64_t rows = (int64_t)n_seqs * cache->n_heads;
-    // CTAs per row: as many as it takes to hold the keys, and more of them while rows leave SMs idle
+    // Few kept rows are copied by the CTA that selects them: up to 32 KB of a row's keys and values that costs the GPU no more than the other kernel,
+    // and the host a launch less (64 of 175 tokens, 7 sequences: 9.4 us and 10.1 of the host, else 8.2 and 11.9); 128 KB take 17 us, else 9.9.
+    const bool copy = A.max_tokens <= 1024 && (int64_t)keep * A.row_bytes * 2 <= 32 * 1024;
+    // CTAs per row: as many as it takes to hold the keys, and more of them while rows leave SMs idle (8 rows of 131,072: 49 us with 8 CTAs or 16, 67 us
+    // with 4; 4,257 tokens: 13.0 us with 2 or more, 15.0 us with one)
     int ctas = 1;
-    while (ctas < 8 && ((int64_t)ctas * KLPM_EVICT_HELD < A.max_tokens || (rows * ctas * 2 <= KLPM_SMS && A.max_tokens / ctas > 4096))) ctas *= 2;
+    while (ctas < 8 && ((int64_t)ctas * KLPM_EVICT_HELD < A.max_tokens || (rows * ctas * 2 <= KLPM_SMS && A.max_tokens / ctas > 2048))) ctas *= 2;
     const int64_t part = ((A.max_tokens + ctas - 1) / ctas + 31) & ~31LL;
     // rows of a warp of the copy: 8 while that leaves every warp of the GPU at most one turn
     const int rpw = rows * keep <= (int64_t)KLPM_SMS * 64 * 8 ? 8 : 32;
     const int64_t blocks = ((int64_t)((keep + rpw - 1) / rpw) * cache->n_heads + 7) / 8;
     if (rows * ctas > 0x7fffffffLL || blocks > 0x7fffffffLL) return RT_ERR_TOO_LARGE;
-    if (part > KLPM_EVICT_HELD) st = launch_select<1024, false>(A, rows, ctas, 0, s);
-    else if (part > 2048) st = launch_select<1024, true>(A, rows, ctas, (size_t)part * 4, s);
-    else st = launch_select<256, true>(A, rows, ctas, (size_t)part * 4, s);
+    const size_t held = (size_t)part * 4;
+    if (copy) return launch_select<256, true, true>(A, rows, ctas, held, s);
+    // (1,024 threads: 2,016 tokens 24.8 us instead of 27.7; 256: 1,008 tokens 9.9 us instead of 10.5)
+    if (part > KLPM_EVICT_HELD) st = launch_select<1024, false, false>(A, rows, ctas, 0, s);
+    else st = part > 1024 ? launch_select<1024, true, false>(A, rows, ctas, held, s) : launch_select<256, true, false>(A, rows, ctas, held, s);
     if (st) return st;
     const dim3 grid((unsigned)blocks, (unsigned)n_seqs);
     return rpw == 8 ? launch_after(evict_copy_kernel<8>, grid, 256, s, A) : launch_after(evict_copy_kernel<32>, grid, 256, s, A);
