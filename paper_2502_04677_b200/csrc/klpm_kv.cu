@@ -380,10 +380,9 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {          // of 16
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
 }
-__device__ __forceinline__ uint32_t e4m3_to_f16(uint32_t two) {           // exact; the low 16 bits hold two values
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));
-    return r;
+__device__ __forceinline__ void e4m3_to_f16(uint32_t four, uint32_t* lo, uint32_t* hi) {           // exact; two values each
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(*lo) : "h"((unsigned short)four));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(*hi) : "h"((unsigned short)(four >> 16)));
 }
 // x and y as the sums of two 16-bit numbers each
 template <bool HALF> __device__ __forceinline__ void split2(float x, float y, uint32_t* hi, uint32_t* lo) {
@@ -466,11 +465,10 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
     const int32_t in_page = (1 << A.c.page_shift) - 1;
     const int my_row = lane / X::CH % TT, my_ch = lane % X::CH;
     // the page of token `lane` of the tile at ci; -1: nothing there
-    auto page_of = [&]() -> int32_t {
-        const int32_t t = ci.tile * TT + lane;
-        if (lane >= TT || t < ci.lo || t >= ci.hi) return -1;
-        const int32_t p = __ldg(A.table + ci.b * A.table_stride + (t >> A.c.page_shift));
-        return (unsigned)p < (unsigned)A.c.n_pages ? p : -1;
+    auto page_of = [&]() -> int32_t {                         // (no branch: a token that is not there looks up one that is)
+        const int32_t t = ci.tile * TT + lane, in = max(ci.lo, min(ci.hi - 1, t));
+        const int32_t p = __ldg(A.table + ci.b * A.table_stride + (in >> A.c.page_shift));
+        return t == in && lane < TT && (unsigned)p < (unsigned)A.c.n_pages ? p : -1;
     };
     int32_t page_next = page_of(), page = -1, at = 0, g_now = 0;           // (at: the lane's token's place in its page)
     int slot_in = 0, tile_in = 0;
@@ -619,20 +617,24 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
         if constexpr (X::E8) {
             unrolled<X::DP / 64>([&](auto h) {
                 constexpr int hb = h.value;
-                if (hb * 64 >= A.c.dim) return;
+                if (X::DP == 256 && hb == 3 && A.c.dim <= 192) return;              // (nothing but zeros)
                 unrolled<TN>([&](auto u) {
                     constexpr int t = u.value, OFF = t * 16 * X::ROW + (hb >> 1) * 128;
                     const uint4 a = lds128<OFF>(key ^ (hb & 1) * 64), b = lds128<OFF + 8 * X::ROW>(key ^ (hb & 1) * 64);
-                    kq(t, hb * 4 + 0, e4m3_to_f16(a.x), e4m3_to_f16(b.x), e4m3_to_f16(a.x >> 16), e4m3_to_f16(b.x >> 16));
-                    kq(t, hb * 4 + 1, e4m3_to_f16(a.y), e4m3_to_f16(b.y), e4m3_to_f16(a.y >> 16), e4m3_to_f16(b.y >> 16));
-                    kq(t, hb * 4 + 2, e4m3_to_f16(a.z), e4m3_to_f16(b.z), e4m3_to_f16(a.z >> 16), e4m3_to_f16(b.z >> 16));
-                    kq(t, hb * 4 + 3, e4m3_to_f16(a.w), e4m3_to_f16(b.w), e4m3_to_f16(a.w >> 16), e4m3_to_f16(b.w >> 16));
+                    const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        uint32_t f[4];
+                        e4m3_to_f16(aw[y], &f[0], &f[2]);
+                        e4m3_to_f16(bw[y], &f[1], &f[3]);
+                        kq(t, hb * 4 + y, f[0], f[1], f[2], f[3]);
+                    }
                 });
             });
         } else {
             unrolled<KS>([&](auto k) {
                 constexpr int ks = k.value;
-                if (ks / 4 * 64 >= A.c.dim) return;
+                if (X::DP == 256 && ks / 4 == 3 && A.c.dim <= 192) return;          // (nothing but zeros)
                 unrolled<TN>([&](auto u) {
                     uint32_t a[4];              // tokens 0-7 and 8-15 of elements 0-7, then of 8-15
                     ldmatrix4<u.value * 16 * X::ROW + ks / 4 * 128>(a, key ^ ks % 4 * 32);
@@ -753,7 +755,8 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
                     for (int y = 0; y < 2; ++y) {
                         const uint32_t sel = y ? 0x7362 : 0x5140;
                         const uint32_t c = __byte_perm(v[0][x / 2], v[1][x / 2], sel), d = __byte_perm(v[2][x / 2], v[3][x / 2], sel);
-                        a[y][0] = e4m3_to_f16(c); a[y][1] = e4m3_to_f16(c >> 16); a[y][2] = e4m3_to_f16(d); a[y][3] = e4m3_to_f16(d >> 16);
+                        e4m3_to_f16(c, &a[y][0], &a[y][1]);
+                        e4m3_to_f16(d, &a[y][2], &a[y][3]);
                     }
                     vp(x, t, a);
                 }
@@ -761,7 +764,7 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
         } else {
             unrolled<KS / 2>([&](auto k) {
                 constexpr int x = k.value * 2;
-                if (x / 4 * 64 >= A.c.dim) return;
+                if (X::DP == 256 && x / 4 == 3 && A.c.dim <= 192) return;
                 unrolled<TN>([&](auto u) {
                     uint32_t a[2][4];           // elements 0-7 and 8-15 of tokens 0-7, then of 8-15
                     ldmatrix4_trans<u.value * 16 * X::ROW + x / 4 * 128>(a[0], value ^ x % 4 * 32);
