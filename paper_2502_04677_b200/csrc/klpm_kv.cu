@@ -314,7 +314,7 @@ template <int TQ_, int TC_, int DP_, int NT_> struct Dec {
     static constexpr int TILE = TT * ROW;                      // bytes of a half tile: keys or values
     static constexpr int CTAS = DP > 128 || NT > 1 ? 2 : 4;      // per SM: what the registers leave room for
     static constexpr int FIT = 192 * 1024 / (CTAS * KLPM_DECODE_WARPS * TILE);
-    static constexpr int RING = FIT < 6 ? FIT : 6;             // half tiles
+    static constexpr int RING = FIT < 5 ? 3 : 5;               // half tiles (an odd number: what is loaded is what is used, some tiles ahead)
     static constexpr int WARP_SMEM = RING * TILE;
     static constexpr int SMEM = KLPM_DECODE_WARPS * WARP_SMEM;
     static constexpr int HEADS = 8 * NT;
@@ -465,10 +465,11 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
     const int32_t in_page = (1 << A.c.page_shift) - 1;
     const int my_row = lane / X::CH % TT, my_ch = lane % X::CH;
     // the page of token `lane` of the tile at ci; -1: nothing there
-    auto page_of = [&]() -> int32_t {                         // (no branch: a token that is not there looks up one that is)
-        const int32_t t = ci.tile * TT + lane, in = max(ci.lo, min(ci.hi - 1, t));
-        const int32_t p = __ldg(A.table + ci.b * A.table_stride + (in >> A.c.page_shift));
-        return t == in && lane < TT && (unsigned)p < (unsigned)A.c.n_pages ? p : -1;
+    auto page_of = [&]() -> int32_t {
+        const int32_t t = ci.tile * TT + lane;
+        int32_t p = -1;
+        if (lane < TT && t >= ci.lo && t < ci.hi) p = __ldg(A.table + ci.b * A.table_stride + (t >> A.c.page_shift));
+        return p < A.c.n_pages ? p : -1;                      // (negative: not there either)
     };
     int32_t page_next = page_of(), page = -1, at = 0, g_now = 0;           // (at: the lane's token's place in its page)
     int slot_in = 0, tile_in = 0;
@@ -541,13 +542,13 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
         if (++slot_out == RING) slot_out = 0;
         return a;
     };
-#pragma unroll
-    for (int i = 0; i < RING - 1; ++i) {
-        if (i & 1) load_values();
-        else load_keys();
-    }
-    for (; left > 0; --left) {
-        if (fresh) {                                          // a row begins, or the span begins inside one
+    // (RING - 1) / 2 tiles ahead: the first rounds only load.  (One copy of the code: a small call runs through it once or twice, and what it
+    // has to fetch of it counts)
+    int ahead = (RING - 1) / 2;
+    uint32_t ph[NT][TN][2], pl[NT][TN][2];
+    for (;;) {
+        const bool live = ahead == 0;
+        if (live && fresh) {                                  // a row begins, or the span begins inside one
             fresh = false;
             begun_here = cc.tile == cc.first;
             heads = min(X::HEADS, A.group - cc.ht * X::HEADS);
@@ -599,19 +600,20 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
             }
         }
         // s = k . q, tokens x heads
-        const uint32_t sk = step();
-        if constexpr (RING & 1) load_keys();
-        else load_values();
-        float s[NT][TN][4], s2[NT][TN][4];                    // (sums of every other step: shorter chains)
+        uint32_t sk = 0;
+        if (live) sk = step();
+        load_keys();
+        if (live) {
+        float s[NT][TN][4], s2[NT][1][4];                     // (one group of tokens: sums of every other step, shorter chains)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int t = 0; t < TN; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[n][t][i] = s2[n][t][i] = 0.0f;
+                for (int i = 0; i < 4; ++i) s[n][t][i] = s2[n][0][i] = 0.0f;
         auto kq = [&](int t, int ks, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma16816<X::HALF>(ks & 1 ? s2[n][t] : s[n][t], a0, a1, a2, a3, qb[n][ks][0], qb[n][ks][1]);
+            for (int n = 0; n < NT; ++n) mma16816<X::HALF>(TN == 1 && ks & 1 ? s2[n][0] : s[n][t], a0, a1, a2, a3, qb[n][ks][0], qb[n][ks][1]);
         };
         const uint32_t key = sk + in_keys;
         if constexpr (X::E8) {
@@ -644,13 +646,12 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
         }
         // p = 2^(s - m): tokens r8 and r8 + 8 of heads 2j and 2j + 1
         const unsigned have = s_there[tile_out++ & 7];
-        uint32_t ph[NT][TN][2], pl[NT][TN][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int t = 0; t < TN; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[n][t][i] = (s[n][t][i] + s2[n][t][i]) * coef[n][i & 1];
+                for (int i = 0; i < 4; ++i) s[n][t][i] = (TN == 1 ? s[n][t][i] + s2[n][0][i] : s[n][t][i]) * coef[n][i & 1];
         if (have != (TT == 32 ? 0xffffffffu : 0xffffu)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -715,10 +716,12 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
                     pl[n][t][i] = transpose8x8(lo);
                 }
         }
+        }
         // o += v . p, elements x heads
-        const uint32_t sv = step();
-        if constexpr (RING & 1) load_values();
-        else load_keys();
+        uint32_t sv = 0;
+        if (live) sv = step();
+        load_values();
+        if (!live) { --ahead; continue; }
         auto vp = [&](int x, int t, const uint32_t (&a)[2][4]) {         // output tiles x, x + 1: the two products of one sum apart from one another
 #pragma unroll
             for (int half = 0; half < 2; ++half)
@@ -788,7 +791,8 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
             finish(cc, begun_here, row_ends, heads, m, l, o);
             fresh = true;
         }
-        if (left > 1) cc.next(A);
+        if (--left == 0) break;
+        cc.next(A);
     }
 }
 
@@ -1105,9 +1109,10 @@ __global__ void __launch_bounds__(WPR == 1 ? 256 : WPR * 32) decode_join_kernel(
 #define KLPM_ROW_WARPS 8
 #define KLPM_ROW_CTAS 16
 template <class X>
-__global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_kernel(const __grid_constant__ DecodeArgs A, int32_t ctas) {
+__global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_kernel(const __grid_constant__ DecodeArgs A, int32_t lg) {       // 2^lg CTAs of a cluster
     using Q = typename Elem<X::TQ>::T;
     constexpr int TT = X::TT, KS = X::KS, NT = X::NT;
+    static_assert(KLPM_ROW_WARPS == 8);
     static_assert(X::PART * 4 <= X::WARP_SMEM, "a warp's result lies in its ring");
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ unsigned s_there[KLPM_ROW_WARPS][8];
@@ -1115,15 +1120,15 @@ __global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_k
     __shared__ float s_lse2[X::HEADS];
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int32_t rank = blockIdx.x % ctas, row = blockIdx.x / ctas;
+    const int32_t ctas = 1 << lg, rank = blockIdx.x & (ctas - 1), row = blockIdx.x >> lg;
     Cursor<X> c;
     c.b = row / A.units;
     c.g = (row - c.b * A.units) / A.head_tiles; c.ht = row - c.b * A.units - c.g * A.head_tiles;
     token_range(A, c.b, &c.lo, &c.hi);
     c.first = c.lo / TT;
     c.end = c.hi > c.lo ? (c.hi + TT - 1) / TT : c.first;
-    const int32_t tiles = c.end - c.first, warps = ctas * KLPM_ROW_WARPS, per = (tiles + warps - 1) / warps;
-    const int32_t parts = per > 0 ? (tiles + per - 1) / per : 0;
+    const int32_t tiles = c.end - c.first, warps = KLPM_ROW_WARPS << lg, per = (tiles + warps - 1) >> (lg + 3);
+    const int32_t parts = per <= 1 ? tiles : (tiles + per - 1) / per;
     const int32_t g = c.g, h0 = c.head(A), heads = min(X::HEADS, A.group - c.ht * X::HEADS);
     clear_ring<X>(A, smem, KLPM_ROW_WARPS * X::WARP_SMEM);
     __syncthreads();
@@ -1140,20 +1145,21 @@ __global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_k
     }
     cluster.sync();
     // output tiles: as many of a CTA's warps to each as there are, a part of the parts to every warp
-    auto part = [&](int k) { return reinterpret_cast<const float*>(cluster.map_shared_rank(smem, k % ctas) + k / ctas * X::WARP_SMEM); };
-    const int share = parts <= 4 ? 1 : max(1, min(KLPM_ROW_WARPS, warps / KS)), at = warp / share;          // (powers of two)
-    const int per_cta = KLPM_ROW_WARPS / share;
-    for (int x0 = rank * per_cta; x0 < KS; x0 += ctas * per_cta) {
-        const int x = x0 + at;
+    auto part = [&](int k) { return reinterpret_cast<const float*>(cluster.map_shared_rank(smem, k & (ctas - 1)) + (k >> lg) * X::WARP_SMEM); };
+    constexpr int LG_KS = X::KS == 4 ? 2 : X::KS == 8 ? 3 : 4;
+    const int lg_share = parts <= 4 ? 0 : max(0, min(3, lg + 3 - LG_KS)), share = 1 << lg_share, mine_of = warp & (share - 1);
+    const int per_cta = KLPM_ROW_WARPS >> lg_share;
+    for (int x0 = rank * per_cta; x0 < X::KS; x0 += ctas * per_cta) {
+        const int x = x0 + (warp >> lg_share);
         Joined<X> J;
         J.clear();
-        if (x < KS) J.template add<4>(x, warp % share, share, parts, part);
+        if (x < X::KS) J.template add<4>(x, mine_of, share, parts, part);
         if (share > 1) {
             J.put(s_all + warp * NT * 2 * 32);
             __syncthreads();
-            if (warp % share == 0) J.take(s_all + warp * NT * 2 * 32, share);
+            if (mine_of == 0) J.take(s_all + warp * NT * 2 * 32, share);
         }
-        if (x < KS && warp % share == 0) write_joined<X>(A, J, c.b, h0, heads, x);
+        if (x < X::KS && mine_of == 0) write_joined<X>(A, J, c.b, h0, heads, x);
         if (share > 1) __syncthreads();
     }
     if (A.weight) {                                           // (one unit per cache head)
@@ -1303,15 +1309,15 @@ template <class X> rt_status launch_decode(DecodeArgs& A, char* work, cudaStream
     const long long tiles = seen / X::TT + 1, units = (long long)A.n_seqs * A.units;
     // CTAs of a cluster: until every warp has a tile or the GPU is full (by half with clusters of 8, by a quarter with 16, which have to
     // find their SMs in one GPC: 16 clusters of 16 take 16.6 us where as many of 8 take 10.3)
-    int ctas = 1;
-    while (ctas < KLPM_ROW_CTAS && ctas * KLPM_ROW_WARPS < tiles
-           && units * ctas * 2 <= KLPM_SMS * (X::CTAS / 2) / (ctas < 4 ? 1 : ctas / 2)) ctas *= 2;
+    int lg = 0;
+    while ((1 << lg) < KLPM_ROW_CTAS && (KLPM_ROW_WARPS << lg) < tiles
+           && (units << (lg + 1)) <= KLPM_SMS * (X::CTAS / 2) / (lg < 2 ? 1 : 1 << (lg - 1))) ++lg;
     // The other kernels start 4.5 us later, but deal out the tiles evenly; a tile per warp takes 1.2 us while the GPU is not full.
     // (128 units: of 65 tiles 22.8 us here, 25.0 us there; of 129 tiles of half the bytes 22.9 us, 19.3 us)
-    if (units * tiles <= 4LL * A.warps && tiles <= (long long)ctas * KLPM_ROW_WARPS * (4 + units * tiles / A.warps) && (!A.weight || A.head_tiles == 1)) {
+    if (units * tiles <= 4LL * A.warps && tiles <= (long long)(KLPM_ROW_WARPS << lg) * (4 + units * tiles / A.warps) && (!A.weight || A.head_tiles == 1)) {
         constexpr int bytes = KLPM_ROW_WARPS * X::WARP_SMEM;
         if (rt_status st = allow_smem<decode_row_kernel<X>>(bytes)) return st;
-        return launch_cluster(decode_row_kernel<X>, (unsigned)(units * ctas), KLPM_ROW_WARPS * 32, ctas, bytes, s, A, (int32_t)ctas);
+        return launch_cluster(decode_row_kernel<X>, (unsigned)(units << lg), KLPM_ROW_WARPS * 32, 1 << lg, bytes, s, A, (int32_t)lg);
     }
     if (rt_status st = allow_smem<decode_kernel<X>>(X::SMEM)) return st;
     decode_kernel<X><<<KLPM_SMS * X::CTAS, KLPM_DECODE_WARPS * 32, X::SMEM, s>>>(A);
