@@ -480,6 +480,7 @@ def kv_rope_table(rot_dim: int, theta: float = 10_000.0, interleaved: bool = Fal
                   original_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda") -> Rope:
     """The frequencies of rotary positions over the first rot_dim elements of a head, scaled for contexts `factor` times as long as
     original_len: scaling "none", "linear", "ntk" or "yarn" (see include/klpm_kv.h)."""
+    _count(rot_dim, "rot_dim")
     if scaling not in ROPE_SCALINGS:
         raise ValueError("scaling must be one of %s" % ", ".join(sorted(ROPE_SCALINGS)))
     turns = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.float64, device=device)
@@ -517,6 +518,13 @@ def _pages(t: torch.Tensor, cache: KvCache, n: int, name: str):
     return t.data_ptr(), stride[0], shape[1]
 
 
+def _count(x: int, name: str) -> int:
+    """A number that fits the C call's int32."""
+    if not 0 <= x < 1 << 31:
+        raise ValueError("%s must be between 0 and 2^31 - 1" % name)
+    return x
+
+
 def kv_rope_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None,
                    rope: Optional[Rope] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> None:
     """Rotate q [n, q_heads, head_dim] into q_out and k by positions (int32[n]), and store k and v [n, n_heads, head_dim] at slots
@@ -543,7 +551,7 @@ def kv_rope_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torc
 
 def kv_decode_workspace(cache: KvCache, n_seqs: int, n_q_heads: int, max_pages: int, with_weight: bool = False) -> torch.Tensor:
     """Device memory for the workspace of a kv_decode of these sizes.  One call uses it at a time."""
-    n = _lib.kv_decode_workspace(cache.p, int(n_seqs), int(n_q_heads), int(max_pages), int(with_weight))
+    n = _lib.kv_decode_workspace(cache.p, _count(n_seqs, "n_seqs"), _count(n_q_heads, "n_q_heads"), _count(max_pages, "max_pages"), int(with_weight))
     if n < 0:
         _check(n, "kv_decode_workspace")
     return torch.empty(max(n, 256), dtype=torch.uint8, device=cache.device)
@@ -577,7 +585,7 @@ def kv_decode(cache: KvCache, q: torch.Tensor, page_table: torch.Tensor, lengths
     elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.device != cache.device:
         raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
     _check(_lib.kv_decode(cache.p, rq, _rows(out, cache, n, "out"), n, table, stride, max_pages, _ints(lengths, cache, n, "lengths"),
-                          cache.head_dim ** -0.5 if scale is None else scale, window, lse.data_ptr() if lse is not None else None, w, ws,
+                          cache.head_dim ** -0.5 if scale is None else scale, _count(window, "window"), lse.data_ptr() if lse is not None else None, w, ws,
                           workspace.data_ptr(), workspace.numel(), _stream_of(cache.device)), "kv_decode")
 
 
@@ -594,6 +602,6 @@ def kv_evict(cache: KvCache, weight: torch.Tensor, page_table: torch.Tensor, len
         raise ValueError("index must be [n_seqs, n_heads, keep]")
     w, ws = _weight(weight, cache, n, max_pages * cache.page_size, "weight")
     nw, nws = _weight(new_weight, cache, n, keep, "new_weight")
-    _check(_lib.kv_evict(cache.p, w, ws, n, table, stride, max_pages, _ints(lengths, cache, n, "lengths"), fresh, fresh_stride, new_pages, keep,
-                         sinks, recent, _ints(index, cache, n * cache.n_heads * keep, "index"), nw, nws, new_weight.shape[2],
+    _check(_lib.kv_evict(cache.p, w, ws, n, table, stride, max_pages, _ints(lengths, cache, n, "lengths"), fresh, fresh_stride, new_pages, _count(keep, "keep"),
+                         _count(sinks, "sinks"), _count(recent, "recent"), _ints(index, cache, n * cache.n_heads * keep, "index"), nw, nws, new_weight.shape[2],
                          _ints(new_lengths, cache, n, "new_lengths"), _stream_of(cache.device)), "kv_evict")

@@ -1319,16 +1319,17 @@ template <class X> rt_status launch_decode(DecodeArgs& A, char* work, cudaStream
         if (rt_status st = allow_smem<decode_row_kernel<X>>(bytes)) return st;
         return launch_cluster(decode_row_kernel<X>, (unsigned)(units << lg), KLPM_ROW_WARPS * 32, 1 << lg, bytes, s, A, (int32_t)lg);
     }
-    if (rt_status st = allow_smem<decode_kernel<X>>(X::SMEM)) return st;
+    const int64_t items = units * X::KS;
+    if (items > 0x7fffffffLL) return RT_ERR_TOO_LARGE;
+    rt_status st = allow_smem<decode_kernel<X>>(X::SMEM);
+    if (st) return st;
     decode_kernel<X><<<KLPM_SMS * X::CTAS, KLPM_DECODE_WARPS * 32, X::SMEM, s>>>(A);
     CK(cudaGetLastError());
     // a unit has A.warps / units parts or so
-    const int64_t items = units * X::KS;
-    if (items > 0x7fffffffLL) return RT_ERR_TOO_LARGE;
     constexpr int MANY = 32 / X::NT;
-    rt_status st = units * 64 <= A.warps   ? launch_after(decode_join_kernel<X, MANY>, dim3((unsigned)items), MANY * 32, s, A)
-                   : units * 16 <= A.warps ? launch_after(decode_join_kernel<X, 8>, dim3((unsigned)items), 256, s, A)
-                                           : launch_after(decode_join_kernel<X, 1>, dim3((unsigned)((items + 7) / 8)), 256, s, A);
+    if (units * 64 <= A.warps) st = launch_after(decode_join_kernel<X, MANY>, dim3((unsigned)items), MANY * 32, s, A);
+    else if (units * 16 <= A.warps) st = launch_after(decode_join_kernel<X, 8>, dim3((unsigned)items), 256, s, A);
+    else st = launch_after(decode_join_kernel<X, 1>, dim3((unsigned)((items + 7) / 8)), 256, s, A);
     if (st || !A.weight) return st;
     return launch_after(decode_weight_kernel<X::TT>, dim3(KLPM_SMS * 4), 256, s, A);
 }
