@@ -104,8 +104,11 @@ int64_t kv_decode_workspace(const kv_cache* cache, int32_t n_seqs, int32_t n_q_h
  *   d_weight  nullable: d_weight[b * weight_stride[0] + g * weight_stride[1] + t] += the sum over the query heads of cache head g of
  *             their softmax weights of token t (max_pages * page_size entries per row; those of masked tokens stay as they are)
  *   q, out    one dtype: the cache's, or either 16-bit type if the cache is KV_E4M3.  They must not overlap.
+ *   n_seqs    at most 65,535 (so for kv_evict)
  *   d_workspace  kv_decode_workspace bytes, aligned to 256; its contents before and after the call mean nothing
- * The result is the same for every call with the same arguments (no atomics on floating-point values). */
+ * The result is the same for every call with the same arguments (no atomics on floating-point values).  Sums are formed before they are divided by
+ * the softmax's sum: the number of tokens times the largest value, times 2^15 for f16 and 8-bit caches, has to stay within 32-bit floating
+ * point.  Infinite and NaN keys or values of tokens that are attended to come out as the formula says. */
 rt_status kv_decode(const kv_cache* cache, const kv_rows* q, const kv_rows* out, int32_t n_seqs, const int32_t* d_page_table,
                     int64_t table_stride, int32_t max_pages, const int32_t* d_lengths, float scale, int32_t window, float* d_lse,
                     float* d_weight, const int64_t* weight_stride, void* d_workspace, int64_t workspace_bytes, void* stream);

@@ -1691,6 +1691,7 @@ int64_t kv_decode_workspace(const kv_cache* cache, int32_t n_seqs, int32_t n_q_h
     if (st) return st;
     if (n_seqs < 0 || n_q_heads < 1 || max_pages < 0 || n_q_heads % cache->n_heads) return RT_ERR_INVALID;
     if (n_seqs > 65535 || n_q_heads > 65535 || (int64_t)max_pages * cache->page_size > KLPM_MAX_TOKENS) return RT_ERR_TOO_LARGE;
+    if ((double)n_seqs * n_q_heads * ((double)max_pages * cache->page_size + 64) > 1e15) return RT_ERR_TOO_LARGE;
     // (the query's type is not known here: the larger of what either needs next to an 8-bit cache)
     int64_t bytes = 0;
     for (int tq = KV_BF16; tq <= KV_F16; ++tq) {
@@ -1711,7 +1712,7 @@ rt_status kv_decode(const kv_cache* cache, const kv_rows* q, const kv_rows* out,
     if (st) return st;
     if (n_seqs < 0 || max_pages < 0 || window < 0 || !(scale == scale) || isinf(scale)) return RT_ERR_INVALID;
     if ((st = check_rows(q, n_seqs)) || (st = check_rows(out, n_seqs))) return st;
-    if (q->dtype == KV_F32 || out->dtype != q->dtype || out->n_heads != q->n_heads) return RT_ERR_INVALID;
+    if (q->dtype == KV_F32 || out->dtype != q->dtype || out->n_heads != q->n_heads || (n_seqs > 0 && q->data == out->data)) return RT_ERR_INVALID;
     if (cache->dtype != KV_E4M3 && cache->dtype != q->dtype) return RT_ERR_INVALID;
     if (q->n_heads % cache->n_heads) return RT_ERR_INVALID;
     if (n_seqs > 65535 || (int64_t)max_pages * cache->page_size > KLPM_MAX_TOKENS) return RT_ERR_TOO_LARGE;
@@ -1749,7 +1750,7 @@ rt_status kv_evict(const kv_cache* cache, const float* d_weight, const int64_t* 
     if (n_seqs > 1 && (table_stride < max_pages || new_stride < new_pages)) return RT_ERR_INVALID;
     if (!weight_stride || !new_weight_stride) return RT_ERR_INVALID;
     if (n_seqs > 0 && (!d_lengths || !d_new_table || !d_index || !d_new_weight || !d_new_lengths)) return RT_ERR_INVALID;
-    if (n_seqs > 0 && max_pages > 0 && (!d_page_table || !d_weight)) return RT_ERR_INVALID;
+    if (n_seqs > 0 && max_pages > 0 && (!d_page_table || !d_weight || d_weight == d_new_weight)) return RT_ERR_INVALID;
     if (n_seqs == 0) return RT_OK;
     EvictArgs A;
     A.c = cache_dev(cache);

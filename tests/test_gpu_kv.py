@@ -438,24 +438,82 @@ def test_decode_the_same_every_time_and_under_a_graph():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
-def test_decode_on_two_streams():
+@pytest.mark.parametrize("wide", [False, True])
+def test_decode_on_two_streams(wide):
     g = gen(12)
     cases = []
     for i, n in enumerate((2500, 4000)):
         table, pages = tables(g, [n, n // 2], 16)
         c = make_cache(g, pages, 16, 2, 64, BF)
         q = torch.randn(2, 8, 64, generator=g, device="cuda").to(BF)
+        table = wide_table(table, 4) if wide else table          # (160,000 tokens)
         cases.append((c, q, table, torch.tensor([n, n // 2], dtype=torch.int32, device="cuda")))
-    want = [check_decode(*x)[0] for x in cases]
+    want = []
+    for c, q, table, lens in cases:
+        out = torch.empty_like(q)
+        K().kv_decode(c, q, table, lens, out)
+        ref, _, _, tol, _, _ = plain_decode(c, q, table, lens, q.shape[2] ** -0.5, 0, None)
+        assert ((out.double() - ref).abs() <= tol).all()
+        want.append(out)
     outs = [[torch.empty_like(x[1]) for _ in range(20)] for x in cases]
+    weights = [torch.zeros(2, 2, x[2].shape[1] * 16, device="cuda") for x in cases]
     streams = [torch.cuda.Stream() for _ in cases]
     torch.cuda.synchronize()
     for k in range(20):
-        for s, x, o in zip(streams, cases, outs):
+        for s, x, o, w in zip(streams, cases, outs, weights):
             with torch.cuda.stream(s):
-                K().kv_decode(*x, o[k], weight=None)
+                K().kv_decode(*x, o[k], weight=w)
     torch.cuda.synchronize()
     assert all(torch.equal(o, w) for got, w in zip(outs, want) for o in got)
+    for w, x in zip(weights, cases):                             # every call added 1 for each of a cache head's four heads
+        assert ((w.double().sum(-1) - 20 * 4).abs() <= 20 * 4 * 1e-4).all()
+
+
+FIRST_CALL = """
+import torch
+from paper_2502_04677_b200 import binding as K
+k, v = (torch.randn(300, 16, 2, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+c = K.KvCache(k, v)
+q = torch.randn(3, 8, 64, device="cuda").to(torch.bfloat16)
+lens = torch.tensor([4000, 17, 300], dtype=torch.int32, device="cuda")
+new = torch.arange(280, 286, dtype=torch.int32, device="cuda").reshape(3, 2)
+x = torch.randn(3, 2, 64, device="cuda").to(torch.bfloat16)
+slots = torch.tensor([4700, 4701, 4702], dtype=torch.int32, device="cuda")
+turned = torch.empty_like(q)
+rope = K.kv_rope_table(64)
+got = []
+for pages in (250, 2500):
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").remainder(250).repeat(3, 1)
+    out, lse = torch.empty_like(q), torch.empty(3, 8, device="cuda")
+    w, nw = torch.zeros(3, 2, pages * 16, device="cuda"), torch.empty(3, 2, 40, device="cuda")
+    index, nl = torch.empty(3, 2, 32, dtype=torch.int32, device="cuda"), torch.empty(3, dtype=torch.int32, device="cuda")
+    def call():
+        K.kv_rope_append(c, x, x, slots, positions=lens, rope=rope, q=q, q_out=turned)
+        K.kv_decode(c, turned, table, lens, out, lse=lse, weight=w)
+        K.kv_evict(c, w, table, lens, new, 32, sinks=2, recent=8, index=index, new_weight=nw, new_lengths=nl)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    graph.replay()
+    torch.cuda.synchronize()
+    seen = [t.clone() for t in (out, lse, w, index, nw, nl)]
+    w.zero_()
+    call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(seen, (out, lse, w, index, nw, nl)))
+    assert torch.isfinite(out).all() and nl.tolist() == [32, 17, 32]
+print("first calls captured")
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    got = subprocess.run([sys.executable, "-c", FIRST_CALL], cwd=root, capture_output=True, text=True, timeout=300)
+    assert got.returncode == 0 and "first calls captured" in got.stdout, got.stderr[-2000:]
 
 
 def test_decode_empty_calls():

@@ -53,7 +53,7 @@ def append(K, c, rope=None, pos=P, slots=P, n=3, q=None, q_out=None, k=None, v=N
     return K.lib().kv_rope_append(at(c), at(rope), pos, slots, n, at(q), at(q_out), at(keep[0]), at(keep[1]), None)
 
 
-def evict(K, c, weight=P, ws=(256, 128), n=3, table=P, table_stride=8, max_pages=8, lengths=P, new=P, new_stride=2, new_pages=2, keep=20, sinks=2,
+def evict(K, c, weight=2 * P, ws=(256, 128), n=3, table=P, table_stride=8, max_pages=8, lengths=P, new=P, new_stride=2, new_pages=2, keep=20, sinks=2,
           recent=4, index=P, nw=P, nws=(256, 128), new_len=128, new_lengths=P):
     a, b = ((ctypes.c_int64 * 2)(*x) if x else None for x in (ws, nws))
     return K.lib().kv_evict(at(c), weight, at(a), n, table, table_stride, max_pages, lengths, new, new_stride, new_pages, keep, sinks, recent, index, nw,
@@ -92,11 +92,13 @@ def test_decode_refusals(K):
     inf = float("inf")
     for bad in [dict(n=-1), dict(max_pages=-1), dict(window=-1), dict(scale=float("nan")), dict(scale=inf), dict(q=rows(K, 3)), dict(q=rows(K, 4, K.KV_F32)),
                 dict(q=rows(K, 4, K.KV_F16), out=rows(K, 4, K.KV_F16)), dict(out=rows(K, 2)), dict(out=rows(K, 4, K.KV_F16)), dict(q=rows(K, 4, data=P + 1)),
-                dict(q=rows(K, 4, data=None)), dict(table=None), dict(lengths=None), dict(table_stride=7), dict(weight=P), dict(work=None),
+                dict(q=rows(K, 4, data=None)), dict(q=rows(K, 4, data=2 * P)), dict(table=None), dict(lengths=None), dict(table_stride=7), dict(weight=P), dict(work=None),
                 dict(work=P + 16), dict(work_bytes=1)]:
         assert decode(K, c, **bad) == K.RT_ERR_INVALID, bad
     assert decode(K, c, max_pages=1 << 27, table_stride=1 << 27) == K.RT_ERR_TOO_LARGE
     assert decode(K, c, n=1 << 17) == K.RT_ERR_TOO_LARGE
+    one = cache(K, n_heads=1, k_stride=(1024, 64, 64), v_stride=(1024, 64, 64))
+    assert K.lib().kv_decode_workspace(at(one), 65535, 65535, 1 << 26, 1) == K.RT_ERR_TOO_LARGE
     assert decode(K, c, n=0) == K.RT_OK
     need = K.lib().kv_decode_workspace(at(c), 3, 4, 8, 1)
     assert need > 0 and decode(K, c, weight=P, ws=(256, 128), work_bytes=need - 1) == K.RT_ERR_INVALID
@@ -118,7 +120,7 @@ def test_evict_refusals(K):
     c = cache(K)
     for bad in [dict(n=-1), dict(max_pages=-1), dict(new_pages=1), dict(keep=0), dict(keep=33), dict(sinks=-1), dict(recent=-1), dict(sinks=17), dict(new_len=19),
                 dict(table_stride=7), dict(new_stride=1), dict(ws=None), dict(nws=None), dict(weight=None), dict(table=None), dict(lengths=None), dict(new=None),
-                dict(index=None), dict(nw=None), dict(new_lengths=None)]:
+                dict(index=None), dict(nw=None), dict(nw=2 * P), dict(new_lengths=None)]:
         assert evict(K, c, **bad) == K.RT_ERR_INVALID, bad
     assert evict(K, c, max_pages=1 << 27, table_stride=1 << 27) == K.RT_ERR_TOO_LARGE
     assert evict(K, c, n=0) == K.RT_OK
@@ -143,3 +145,10 @@ def test_the_binding_refuses_cpu_tensors(K):
     x = torch.zeros(2, 4, 1, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         K.KvCache(x, x)
+
+
+def test_the_binding_refuses_numbers_that_do_not_fit(K):
+    for x in (-1, 1 << 31, 1 << 40):
+        with pytest.raises(ValueError):
+            K._count(x, "window")
+    assert K._count((1 << 31) - 1, "window") == (1 << 31) - 1
