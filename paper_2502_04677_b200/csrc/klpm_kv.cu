@@ -1377,12 +1377,13 @@ __device__ __forceinline__ unsigned evict_key(const EvictArgs& A, int32_t b, int
 }
 
 // Copies `rows` kept rows of cache head g, keys and values: lane r holds where row r is (sk, sv) and goes (dk, dv; byte offsets, sk < 0: nothing
-// to copy).  16 bytes a lane, eight loads in flight.
+// to copy).  16 bytes a lane, four loads in flight (eight leave fewer warps on an SM: 32
+// sequences of up to 8,191 tokens take 152.5 us then, else 150).
 __device__ __forceinline__ void copy_kept(const EvictArgs& A, int rows, int64_t sk, int64_t sv, int64_t dk, int64_t dv) {
     const int lane = threadIdx.x & 31;
     const unsigned slots = A.row_bytes / 8;        // 16-byte pieces of a row's key and value together, at most 64
     const unsigned magic = (1u << 20) / slots + 1; // e * magic >> 20 = e / slots for e < 2^20 / slots
-    constexpr int DEEP = 8;
+    constexpr int DEEP = 4;
     for (unsigned e0 = 0; e0 < rows * slots; e0 += 32 * DEEP) {
         int4 v[DEEP];
         char* to[DEEP];
@@ -1561,16 +1562,27 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const EvictArgs A, int3
         for (int r = 0; r < rank; ++r) { gts += *cluster.map_shared_rank(&S.gt, r); eqs += *cluster.map_shared_rank(&S.eq, r); }
         cluster.barrier_arrive();               // nobody leaves while its shared memory is read
     }
-    if (K > 0)
-        for (int32_t t = a0; t < a1; t += 32) {
-            const unsigned k = t + lane < a1 ? key(t + lane) : 0u;
+    constexpr int AHEAD = COPY ? 1 : 2;          // groups of 32 tokens whose weights are in flight
+    for (int32_t base = a0; base < a1 && K > 0; base += 32 * AHEAD) {
+        unsigned key_of[AHEAD];
+        float weight_of[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int32_t t = base + 32 * i + lane;
+            key_of[i] = t < a1 ? key(t) : 0u;
+            weight_of[i] = key_of[i] && key_of[i] >= limit ? __ldg(w + t) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int32_t t = base + 32 * i;
+            const unsigned k = key_of[i];
             const bool gt = k > limit, eq = k == limit && k;
             const unsigned bg = __ballot_sync(FULL_MASK, gt), be = __ballot_sync(FULL_MASK, eq), below = (1u << lane) - 1;
             const int32_t e = eqs + __popc(be & below), j = gts + __popc(bg & below) + min(e, want);
             const bool kept = gt || (eq && e < want);
             if (kept) {
                 index[j] = t + lane;
-                nw[j] = __ldg(w + t + lane);
+                nw[j] = weight_of[i];
             }
             if constexpr (COPY) {
                 const unsigned bk = __ballot_sync(FULL_MASK, kept);
@@ -1589,15 +1601,16 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const EvictArgs A, int3
             gts += __popc(bg);
             eqs += __popc(be);
         }
+    }
     for (int32_t j = K + rank * T + tid; j < A.keep; j += ctas * T) index[j] = -1;
     for (int32_t j = K + rank * T + tid; j < A.new_len; j += ctas * T) nw[j] = 0.0f;
     if (g == 0 && rank == 0 && tid == 0) A.new_lengths[b] = K;
     if (ctas > 1) cluster.barrier_wait();
 }
 
-// The kept rows, keys and values: a warp looks up ROWS of them, one per lane, then copies them 16 bytes a lane, eight loads in flight.
+// The kept rows, keys and values: a warp looks up ROWS of them, one per lane, then copies them.
 template <int ROWS>
-__global__ void __launch_bounds__(256) evict_copy_kernel(const EvictArgs A) {
+__global__ void __launch_bounds__(256, 5) evict_copy_kernel(const EvictArgs A) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const int64_t id = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -1765,7 +1778,7 @@ rt_status kv_evict(const kv_cache* cache, const float* d_weight, const int64_t* 
     // Few kept rows are copied by the CTA that selects them: up to 32 KB of a row's keys and values that costs the GPU no more than the other kernel,
     // and the host a launch less (64 of 175 tokens, 7 sequences: 9.4 us and 10.1 of the host, else 8.2 and 11.9); 128 KB take 17 us, else 9.9.
     const bool copy = A.max_tokens <= 1024 && (int64_t)keep * A.row_bytes * 2 <= 32 * 1024;
-    // CTAs per row: as many as it takes to hold the keys, and more of them while rows leave SMs idle (8 rows of 131,072: 49 us with 8 CTAs or 16, 67 us
+    // CTAs per row: as many as it takes to hold the keys, and more of them while rows leave SMs idle (8 rows of 131,072: 46 us with 8 CTAs, 49 with 16, 67
     // with 4; 4,257 tokens: 13.0 us with 2 or more, 15.0 us with one)
     int ctas = 1;
     while (ctas < 8 && ((int64_t)ctas * KLPM_EVICT_HELD < A.max_tokens || (rows * ctas * 2 <= KLPM_SMS && A.max_tokens / ctas > 2048))) ctas *= 2;
