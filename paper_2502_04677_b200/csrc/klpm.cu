@@ -387,7 +387,8 @@ __device__ __forceinline__ int32_t walk_chain(const TreeDev& T, const int32_t* _
 }
 
 // Where the tokens of a match are in the pool, one CTA per query: the edges from the node where the match ended up to the
-// root.  Bound by the chain of parents (one dependent trip per node) for few queries, by the writes for many.
+// root.  Bound by the chain of parents (one dependent trip per node) for few queries, by the writes for many (medium configuration: 8,192 queries of
+// up to 4,094 tokens 37 us, 32 of them 2.7 us; 32 queries at the ends of trunks cut a hundred times 64 us).
 __global__ void __launch_bounds__(256) prefix_slots_kernel(const TreeDev T, const int32_t* __restrict__ tnode,
                                                            const int32_t* __restrict__ mlen, int32_t* __restrict__ slots,
                                                            int64_t row_stride, int32_t max_len) {

@@ -735,6 +735,17 @@ def test_a_step_of_an_engine(budget):
     width = int(m.max())
     slots = torch.zeros(n, width, dtype=torch.int32, device="cuda")
     B.rt_prefix_slots(tree, node, m, slots)
+    # one slot, one prefix: a slot says which token came last and which slot the one before it has, and the other way round
+    after, came_from = {}, {}
+    toks, offs = qt.tolist(), qo.tolist()
+    for i, row in enumerate(slots.tolist()):
+        before = -1
+        for d in range(int(m[i])):
+            assert 0 <= row[d] < cap
+            step = (before, toks[offs[i] + d])
+            assert after.setdefault(step, row[d]) == row[d] and came_from.setdefault(row[d], step) == step
+            before = row[d]
+        assert row[int(m[i]):] == [-1] * (width - int(m[i]))
     # keys and values of a token go by its prefix: here by its slot, as two prompts share a slot exactly where they share the prefix
     g = gen(21)
     ks, vs = (torch.randn(cap, h, dim, generator=g, device="cuda").to(BF) for _ in range(2))
