@@ -1316,9 +1316,11 @@ template <class X> rt_status launch_decode(DecodeArgs& A, char* work, cudaStream
     int lg = 0;
     while ((1 << lg) < KLPM_ROW_CTAS && (KLPM_ROW_WARPS << lg) < tiles
            && (units << (lg + 1)) <= KLPM_SMS * (X::CTAS / 2) / (lg < 2 ? 1 : 1 << (lg - 1))) ++lg;
-    // The other kernels start 4.5 us later, but deal out the tiles evenly; a tile per warp takes 1.2 us while the GPU is not full.
-    // (128 units: of 65 tiles 22.8 us here, 25.0 us there; of 129 tiles of half the bytes 22.9 us, 19.3 us)
-    if (units * tiles <= 4LL * A.warps && tiles <= (long long)(KLPM_ROW_WARPS << lg) * (4 + units * tiles / A.warps) && (!A.weight || A.head_tiles == 1)) {
+    // The other kernels start 3 to 7 us later, but deal out the tiles evenly; here the longest row counts, and every cluster more than the GPU holds
+    // at once.  Over 40 calls of all kinds (here, there): 24 rows of 208 tiles, 6.5 a warp 17.7, 22.5 us; 8 of 755, 11.8 a warp 19.9, 19.1; 128
+    // of 129 22.9, 19.3; 200 of 39 17.2, 21.2; 312 of 27 32.4, 29.3; 872 of 8 26.3, 22.0; 608 of 4 where 148 fit 37.5, 21.1.
+    const long long load = units * tiles / A.warps;
+    if (units <= KLPM_SMS * (X::CTAS / 2) && load <= 4 && tiles <= (long long)(KLPM_ROW_WARPS << lg) * (6 + load) && (!A.weight || A.head_tiles == 1)) {
         constexpr int bytes = KLPM_ROW_WARPS * X::WARP_SMEM;
         if (rt_status st = allow_smem<decode_row_kernel<X>>(bytes)) return st;
         return launch_cluster(decode_row_kernel<X>, (unsigned)(units << lg), KLPM_ROW_WARPS * 32, 1 << lg, bytes, s, A, (int32_t)lg);
