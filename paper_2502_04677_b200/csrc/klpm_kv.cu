@@ -140,24 +140,38 @@ struct AppendArgs {
     const int32_t *pos, *slot;
     int32_t n, rot, interleaved;
     float factor;
-    int32_t units, slices;        // per token: units of a head (pairs, or 16 elements), threads that share its heads
+    int32_t units;                // of a head: pairs, or 16 elements
+    int32_t slices, tokens;       // of a CTA: threads that share a token's heads (in each of gridDim.y CTAs), tokens
 };
 
 // (a, b) -> (a cos - b sin, a sin + b cos) for the pairs of a head, angle = position x turns x 2 pi.  One thread handles one unit of a head -- a
-// pair of elements, or (VEC) 8 pairs in 16 elements that two 16-byte loads bring -- of every `slices`-th head of a token, so that the angles
-// of its pairs are worked out once.  Bound by HBM for many tokens (32,768 of 32 + 2 x 8 heads of 128, bf16: 136.5 us, 5.9 TB/s of what has to
-// be read and written), by the launch and three dependent loads for few (1 token 2.7 us, 193 into an 8-bit cache 3.9 us).
+// pair of elements, or (VEC) 8 pairs in 16 elements that two 16-byte loads bring -- of some of a token's heads.  A CTA works out the angles of its
+// tokens once, in shared memory (64-bit products, a sine and a cosine each: with every thread at its own, 300 tokens of 12 heads took
+// 4.5 us instead of 3.0).  Bound by HBM for many tokens (32,768 of 32 + 2 x 8 heads of 128, bf16: 137.7 us, 5.9 TB/s of what has to
+// be read and written), by the launch and three dependent loads for few (1 token 2.4 us, 193 into an 8-bit cache 3.4 us).
 template <int TX, int TC, bool VEC>
 __global__ void __launch_bounds__(256) rope_append_kernel(const AppendArgs A) {
     using X = typename Elem<TX>::T;
     using C = typename Elem<TC>::T;
     constexpr int P = VEC ? 8 : 1;
-    const int64_t gid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    const int32_t per = A.units * A.slices;
-    const int32_t tok = (int32_t)(gid / per);
-    if (tok >= A.n) return;
-    const int32_t r = (int32_t)(gid - (int64_t)tok * per);
+    extern __shared__ float2 s_turned[];          // [tokens][rot / 2] cosine and sine
+    const int tid = threadIdx.x, per = A.units * A.slices, half = A.turns ? A.rot / 2 : 0;
+    const int64_t t0 = (int64_t)blockIdx.x * A.tokens;
+    const int mine = tid / per, r = tid - mine * per;         // the token of this CTA's
     const int32_t slice = r / A.units, u = r - slice * A.units;
+    for (int i = tid; i < A.tokens * half; i += 256) {
+        const int which = i / half, pair = i - which * half;
+        if (t0 + which >= A.n) break;
+        // whole turns are taken off in 64 bits: what is left of a far position is exact to 2^-31 * 2^-22 of a turn and better
+        double t = (double)__ldg(A.pos + t0 + which) * __ldg(A.turns + pair);
+        t -= rint(t);
+        float sn, cs;
+        sincospif(2.0f * (float)t, &sn, &cs);
+        s_turned[i] = make_float2(cs * A.factor, sn * A.factor);
+    }
+    __syncthreads();
+    const int64_t tok = t0 + mine;
+    if (mine >= A.tokens || tok >= A.n) return;
     // The unit's elements: P from e0 and P from e1 on, half of the rotated elements (or half of the others) apart, so that neighbouring
     // threads are neighbours in memory.  Pairs are (e0 + j, e1 + j), or if interleaved neighbours in each of the two (VEC) or e0, e0 + 1.
     const int32_t rot_units = A.turns ? A.rot / (2 * P) : 0;
@@ -169,23 +183,18 @@ __global__ void __launch_bounds__(256) rope_append_kernel(const AppendArgs A) {
 #pragma unroll
     for (int j = 0; j < P; ++j) { cs[j] = 1.0f; sn[j] = 0.0f; }
     if (turn) {
-        const double p = (double)__ldg(A.pos + tok);
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            // whole turns are taken off in 64 bits: what is left of a far position is exact to 2^-31 * 2^-22 of a turn and better
             const int32_t pair = !VEC || !A.interleaved ? u * P + j : j < P / 2 ? e0 / 2 + j : e1 / 2 + j - P / 2;
-            double t = p * __ldg(A.turns + pair);
-            t -= rint(t);
-            float s, c;
-            sincospif(2.0f * (float)t, &s, &c);
-            cs[j] = c * A.factor; sn[j] = s * A.factor;
+            const float2 f = s_turned[mine * half + pair];
+            cs[j] = f.x; sn[j] = f.y;
         }
     }
     const int32_t slot = __ldg(A.slot + tok);
     const int32_t page = slot >> A.c.page_shift, at = slot & ((1 << A.c.page_shift) - 1);
     const bool stored = slot >= 0 && page < A.c.n_pages;
     const int32_t heads = A.q.heads + A.k.heads + A.v.heads;
-    for (int32_t h = slice; h < heads; h += A.slices) {
+    for (int32_t h = blockIdx.y * A.slices + slice; h < heads; h += A.slices * gridDim.y) {
         const bool is_q = h < A.q.heads, is_v = h >= A.q.heads + A.k.heads;
         if (!is_q && !stored) break;
         const RowsDev& R = is_q ? A.q : is_v ? A.v : A.k;
@@ -253,9 +262,9 @@ __global__ void __launch_bounds__(256) rope_append_kernel(const AppendArgs A) {
     }
 }
 
-template <int TX, int TC> void launch_append(const AppendArgs& A, bool vec, unsigned grid, cudaStream_t s) {
-    if (vec) rope_append_kernel<TX, TC, true><<<grid, 256, 0, s>>>(A);
-    else rope_append_kernel<TX, TC, false><<<grid, 256, 0, s>>>(A);
+template <int TX, int TC> void launch_append(const AppendArgs& A, bool vec, dim3 grid, size_t smem, cudaStream_t s) {
+    if (vec) rope_append_kernel<TX, TC, true><<<grid, 256, smem, s>>>(A);
+    else rope_append_kernel<TX, TC, false><<<grid, 256, smem, s>>>(A);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1688,21 +1697,27 @@ rt_status kv_rope_append(const kv_cache* cache, const kv_rope* rope, const int32
     const bool vec = A.c.dim % 16 == 0 && A.rot % 16 == 0 && rows_aligned(k) && rows_aligned(v) && (!q || (rows_aligned(q) && rows_aligned(q_out)));
     A.units = A.c.dim / (vec ? 16 : 2);
     const int32_t heads = A.q.heads + A.k.heads + A.v.heads;
-    // Threads that share a token's heads: each works out the angles anew, but few tokens need many threads.  48 heads of 128 elements, with one head
-    // a thread, a quarter of the heads, 12 heads: 193 tokens 4.1, 4.6, - us; 1,000: 11.6, 8.6, - us; 3,000: 28.7, 18.8, 19.2 us; 32,768: 278, 157, 138 us
-    A.slices = n < 256 ? heads : n < 4096 ? (heads + 3) / 4 : (heads < 4 ? heads : 4);
-    const int64_t blocks = ((int64_t)n * A.units * A.slices + 255) / 256;
-    if (blocks > 0x7fffffffLL) return RT_ERR_TOO_LARGE;
+    // Heads per thread: one while that leaves the GPU room, up to a quarter of them (12 of 48) where there is enough to do without.  48 heads of 128
+    // elements with 1, 2, 3, 12 heads a thread: 300 tokens 5.3, 3.8, 4.3, 8.0 us; 1,000 11.9, 9.1, 7.3, 13.3; 12,000 113, 81, 62, 56
+    const int64_t items = (int64_t)n * heads * (A.c.dim / 16);
+    const int32_t limit = heads < 8 ? 2 : heads / 4, wanted = items < 90000 ? 1 : items < 170000 ? 2 : items < 1000000 ? 3 : limit;
+    const int32_t each = wanted < limit ? wanted : limit;
+    const int32_t all = (heads + each - 1) / each, most = 256 / A.units, groups = (all + most - 1) / most;
+    A.slices = (all + groups - 1) / groups;
+    A.tokens = 256 / (A.units * A.slices);
+    const int64_t blocks = ((int64_t)n + A.tokens - 1) / A.tokens;
+    if (blocks > 0x7fffffffLL || groups > 65535) return RT_ERR_TOO_LARGE;
+    const size_t smem = (size_t)A.tokens * (A.rot / 2) * sizeof(float2);
     cudaStream_t s = (cudaStream_t)stream;
-    const unsigned grid = (unsigned)blocks;
+    const dim3 grid((unsigned)blocks, (unsigned)groups);
     switch (k->dtype * 4 + cache->dtype) {
-        case KV_F32 * 4 + KV_BF16: launch_append<KV_F32, KV_BF16>(A, vec, grid, s); break;
-        case KV_F32 * 4 + KV_F16: launch_append<KV_F32, KV_F16>(A, vec, grid, s); break;
-        case KV_F32 * 4 + KV_E4M3: launch_append<KV_F32, KV_E4M3>(A, vec, grid, s); break;
-        case KV_BF16 * 4 + KV_BF16: launch_append<KV_BF16, KV_BF16>(A, vec, grid, s); break;
-        case KV_BF16 * 4 + KV_E4M3: launch_append<KV_BF16, KV_E4M3>(A, vec, grid, s); break;
-        case KV_F16 * 4 + KV_F16: launch_append<KV_F16, KV_F16>(A, vec, grid, s); break;
-        default: launch_append<KV_F16, KV_E4M3>(A, vec, grid, s); break;
+        case KV_F32 * 4 + KV_BF16: launch_append<KV_F32, KV_BF16>(A, vec, grid, smem, s); break;
+        case KV_F32 * 4 + KV_F16: launch_append<KV_F32, KV_F16>(A, vec, grid, smem, s); break;
+        case KV_F32 * 4 + KV_E4M3: launch_append<KV_F32, KV_E4M3>(A, vec, grid, smem, s); break;
+        case KV_BF16 * 4 + KV_BF16: launch_append<KV_BF16, KV_BF16>(A, vec, grid, smem, s); break;
+        case KV_BF16 * 4 + KV_E4M3: launch_append<KV_BF16, KV_E4M3>(A, vec, grid, smem, s); break;
+        case KV_F16 * 4 + KV_F16: launch_append<KV_F16, KV_F16>(A, vec, grid, smem, s); break;
+        default: launch_append<KV_F16, KV_E4M3>(A, vec, grid, smem, s); break;
     }
     CK(cudaGetLastError());
     return RT_OK;
