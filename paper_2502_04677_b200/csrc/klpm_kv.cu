@@ -593,9 +593,11 @@ __device__ __forceinline__ void decode_span(const DecodeArgs& A, uint32_t ring, 
                     most = fmaxf(most, __shfl_xor_sync(FULL_MASK, most, 2));
                     int e = 0;
                     if (most > 0.0f) frexpf(most, &e);
-                    e = max(-110, min(110, 15 - e));
+                    // (-113: the largest elements, from 2^127 on, become 2^14 and more; with 110 the smallest, 2^-133, are f16's 2^-23.  64 bits, as
+                    // the scale that goes with such queries may be subnormal)
+                    e = max(-113, min(110, 15 - e));
                     const float up = ldexpf(1.0f, e);
-                    c = ldexpf(c, -e);
+                    c = (float)((double)A.scale * A.c.k_scale * 1.4426950408889634 * (double)ldexpf(1.0f, -e));
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
