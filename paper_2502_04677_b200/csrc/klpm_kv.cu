@@ -907,37 +907,157 @@ template <class X> struct Joined {
             }
     }
 };
-// Elements of an output tile that came out as NaN although the scores are numbers, by one warp: an infinite value times the second half of
-// a probability, which may be 0 or negative, is no number, while the sum of p_t v_t is infinite.  They are summed with whole
-// probabilities, one token after the other.
-template <class X> __device__ __noinline__ void decode_repair(const DecodeArgs& A, int32_t b, int32_t h, int x, float lse2) {
+// Elements of output tile x that came out as NaN although the scores are numbers.  A value that is NaN makes them so, and they stay; but an infinite
+// value times the second half of a probability, which may be 0 or negative, is no number either, while the sum of p_t v_t is infinite, and so is any value of a
+// token whose score is -inf times its 0.  bad: the heads (h0 + bit) with such elements; norm: lane h's base-2 logarithm of the softmax's sum of head h.
+//   - What is not finite among the values of tokens that take part says what an element is: NaN, the infinity if there is one sign of it, NaN with both.
+//     The values alone are read, a token per lane; scores only of a group of tokens with something new, to leave out those of -inf.  It ends as soon as every
+//     element is known to be NaN.
+//   - Elements with nothing of that kind are summed again with whole probabilities.
+// WARPS: of the CTA, which take turns with groups of tokens (all of them call this, behind a barrier); 1: a warp by itself.  8-bit values are finite or NaN, which is
+// what comes out anyway.  A NaN at the end of a row: 2 sequences of 131,072 tokens (bf16, 2 cache heads of 128) 396 us instead of 70, one of 20,000 tokens 86 instead
+// of 28, 200 of 2,000 172 instead of 87.
+template <int WARPS> struct RepairShared {
+    float sum[WARPS][16];
+    unsigned flag[16][2];
+};
+template <class X, int WARPS>
+__device__ __noinline__ void decode_repair(const DecodeArgs& A, int32_t b, int32_t h0, unsigned bad, float norm, int x, RepairShared<WARPS>* S) {
     using Q = typename Elem<X::TQ>::T;
     using C = typename Elem<X::TC>::T;
-    const int lane = threadIdx.x & 31;
-    const int32_t g = h / A.group;
-    const int d = out_element<X>(x, lane & 7, (lane >> 3) & 1);             // of lanes 0-15
-    const Q* q = reinterpret_cast<const Q*>(A.q.p + b * A.q.sr + h * A.q.sh);
-    Q* out = reinterpret_cast<Q*>(A.out.p + b * A.out.sr + h * A.out.sh);
-    float o = 0.0f;
+    static_assert(!X::E8 && sizeof(C) == 2 && X::HEADS <= 16);
+    constexpr unsigned EXPONENT = X::HALF ? 0x7c00u : 0x7f80u, CARRY = 0x8000u - EXPONENT;
+    constexpr int DEEP = 4;                                  // groups of 32 tokens in flight
+    const int lane = threadIdx.x & 31, warp = WARPS > 1 ? threadIdx.x >> 5 : 0;
+    const int32_t g = h0 / A.group, d0 = x * 16;
+    const bool second = d0 + 8 < A.c.dim;                    // (dim is a multiple of 8)
+    __syncwarp();
+    unsigned want = 0;                                       // lane h: which of the tile's elements of head h are NaN
+    for (unsigned rest = bad; rest; rest &= rest - 1) {
+        const int hd = __ffs(rest) - 1;
+        const Q* out = reinterpret_cast<const Q*>(A.out.p + b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
+        const float y = lane < 16 && d0 + lane < A.c.dim ? to_float(out[d0 + lane]) : 0.0f;
+        const unsigned m = __ballot_sync(FULL_MASK, y != y);
+        if (lane == hd) want = m;
+    }
     int32_t lo, hi;
     token_range(A, b, &lo, &hi);
-    for (int32_t t = lo; t < hi; ++t) {
-        const int32_t page = __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift));
-        if ((unsigned)page >= (unsigned)A.c.n_pages) continue;
-        const int32_t at = t & ((1 << A.c.page_shift) - 1);
-        const C* k = reinterpret_cast<const C*>(A.c.k + page * A.c.ks[0] + at * A.c.ks[1] + g * A.c.ks[2]);
-        const C* v = reinterpret_cast<const C*>(A.c.v + page * A.c.vs[0] + at * A.c.vs[1] + g * A.c.vs[2]);
+    auto page_of = [&](int32_t t) -> int32_t {
+        const int32_t p = t < hi ? __ldg(A.table + b * A.table_stride + (t >> A.c.page_shift)) : -1;
+        return p < A.c.n_pages ? p : -1;
+    };
+    auto load = [&](int32_t t, int32_t page, uint4 (&v)[2]) {
+        v[0] = v[1] = make_uint4(0, 0, 0, 0);
+        if (page < 0) return;
+        const char* p = A.c.v + page * A.c.vs[0] + (t & ((1 << A.c.page_shift) - 1)) * A.c.vs[1] + g * A.c.vs[2] + d0 * 2;
+        v[0] = *reinterpret_cast<const uint4*>(p);
+        if (second) v[1] = *reinterpret_cast<const uint4*>(p + 16);
+    };
+    auto score = [&](int hd, int32_t t, int32_t page) -> float {           // of this lane's token, base 2
+        const Q* q = reinterpret_cast<const Q*>(A.q.p + b * A.q.sr + (int64_t)(h0 + hd) * A.q.sh);
+        const char* k = A.c.k + page * A.c.ks[0] + (t & ((1 << A.c.page_shift) - 1)) * A.c.ks[1] + g * A.c.ks[2];
         float s = 0.0f;
-        for (int i = lane; i < A.c.dim; i += 32) s += to_float(q[i]) * to_float(k[i]);
-        for (int w = 16; w; w >>= 1) s += __shfl_xor_sync(FULL_MASK, s, w);
-        s *= A.scale * A.c.k_scale * 1.4426950408889634f;
-        if (s != -INFINITY && d < A.c.dim) o += exp2f(s - lse2) * to_float(v[d]);
+#pragma unroll 4
+        for (int32_t d = 0; d < A.c.dim; d += 8) {
+            alignas(16) C e[8];
+            *reinterpret_cast<uint4*>(e) = *reinterpret_cast<const uint4*>(k + d * 2);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += to_float(q[d + i]) * to_float(e[i]);
+        }
+        return s * (A.scale * A.c.k_scale * 1.4426950408889634f);
+    };
+    // lane h: what is not finite among the values that head h attends to -- bits 0-15 of inf: +infinity, 16-31: -infinity, of nan: NaN
+    unsigned inf = 0, nan = 0;
+    auto open = [&]() { return want & ~(nan | (inf & inf >> 16)); };
+    for (int32_t t0 = lo + warp * 32 * DEEP; t0 < hi; t0 += WARPS * 32 * DEEP) {
+        int32_t page[DEEP];
+        uint4 v[DEEP][2];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) page[i] = page_of(t0 + i * 32 + lane);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) load(t0 + i * 32 + lane, page[i], v[i]);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            const unsigned w[8] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w, v[i][1].x, v[i][1].y, v[i][1].z, v[i][1].w};
+            unsigned any = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) any |= (w[j] & EXPONENT * 0x10001u) + CARRY * 0x10001u;
+            if (!__any_sync(FULL_MASK, any & 0x80008000u)) continue;
+            unsigned mine_inf = 0, mine_nan = 0;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const unsigned u = w[j >> 1] >> (j & 1) * 16 & 0xffffu;
+                if ((u & EXPONENT) != EXPONENT) continue;
+                if (u & (CARRY - 1)) mine_nan |= 1u << j;
+                else mine_inf |= (u & 0x8000u ? 0x10000u : 1u) << j;
+            }
+            const unsigned all_inf = __reduce_or_sync(FULL_MASK, mine_inf), all_nan = __reduce_or_sync(FULL_MASK, mine_nan);
+            const unsigned more = all_inf & ~inf;
+            for (unsigned need = __ballot_sync(FULL_MASK, (more | more >> 16 | all_nan) & open()); need; need &= need - 1) {
+                const int hd = __ffs(need) - 1;
+                const bool there = (mine_inf | mine_nan) && score(hd, t0 + i * 32 + lane, page[i]) != -INFINITY;
+                const unsigned a = __reduce_or_sync(FULL_MASK, there ? mine_inf : 0u), n = __reduce_or_sync(FULL_MASK, there ? mine_nan : 0u);
+                if (lane == hd) { inf |= a; nan |= n; }
+            }
+        }
+        if (!__any_sync(FULL_MASK, open())) break;
     }
-    __syncwarp();
-    if (lane < 16 && d < A.c.dim && to_float(out[d]) != to_float(out[d])) out[d] = from_float<Q>(o * A.c.v_scale);
+    if constexpr (WARPS > 1) {
+        if (threadIdx.x < 16) S->flag[threadIdx.x][0] = S->flag[threadIdx.x][1] = 0;
+        __syncthreads();
+        if (lane < 16 && inf) atomicOr(&S->flag[lane][0], inf);
+        if (lane < 16 && nan) atomicOr(&S->flag[lane][1], nan);
+        __syncthreads();
+        if (lane < 16) { inf = S->flag[lane][0]; nan = S->flag[lane][1]; }
+    }
+    for (unsigned rest = bad; rest; rest &= rest - 1) {
+        const int hd = __ffs(rest) - 1;
+        const unsigned w = __shfl_sync(FULL_MASK, want, hd), f = __shfl_sync(FULL_MASK, inf, hd), n = __shfl_sync(FULL_MASK, nan, hd);
+        const float lse2 = __shfl_sync(FULL_MASK, norm, hd);
+        float y = 0.0f;
+        if (w & ~(n | f | f >> 16)) {
+            float o[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[j] = 0.0f;
+            for (int32_t t0 = lo + warp * 32; t0 < hi; t0 += WARPS * 32) {
+                const int32_t t = t0 + lane, page = page_of(t);
+                if (page < 0) continue;
+                const float s = score(hd, t, page);
+                if (s == -INFINITY) continue;
+                const float p = exp2f(s - lse2);
+                uint4 v[2];
+                load(t, page, v);
+                const unsigned u[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const uint16_t bits = (uint16_t)(u[j >> 1] >> (j & 1) * 16);
+                    o[j] += p * to_float(*reinterpret_cast<const C*>(&bits));
+                }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                for (int d = 16; d; d >>= 1) o[j] += __shfl_xor_sync(FULL_MASK, o[j], d);
+                if (lane == j) y = o[j];
+            }
+            if constexpr (WARPS > 1) {
+                if (lane < 16) S->sum[warp][lane] = y;
+                __syncthreads();
+                y = 0.0f;
+                for (int k = 0; k < WARPS && lane < 16; ++k) y += S->sum[k][lane];
+                __syncthreads();
+            }
+        }
+        const unsigned bit = 1u << (lane & 15);
+        if ((f & bit) || (f >> 16 & bit)) y = f & bit ? INFINITY : -INFINITY;
+        if (warp == 0 && lane < 16 && (w & bit) && !(n & bit) && !(f & f >> 16 & bit))
+            reinterpret_cast<Q*>(A.out.p + b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh)[d0 + lane] = from_float<Q>(y);
+    }
+    if constexpr (WARPS > 1) __syncthreads();
 }
-// The outputs of tile x of a unit whose parts are joined; what a warp writes here nobody else writes.
-template <class X> __device__ __forceinline__ void write_joined(const DecodeArgs& A, const Joined<X>& J, int32_t b, int32_t h0, int32_t heads, int x) {
+// The outputs of tile x of a unit whose parts are joined; what a warp writes here nobody else writes.  Returns the heads that decode_repair has to look at, and
+// their logarithms of the softmax's sum in *norm.
+template <class X> __device__ __forceinline__ unsigned write_joined(const DecodeArgs& A, const Joined<X>& J, int32_t b, int32_t h0, int32_t heads, int x, float* norm) {
     using Q = typename Elem<X::TQ>::T;
     const int lane = threadIdx.x & 31, r8 = lane >> 2, j = lane & 3;
     unsigned bad = 0;                                        // heads with a NaN among this lane's elements
@@ -954,7 +1074,7 @@ template <class X> __device__ __forceinline__ void write_joined(const DecodeArgs
                 const int d = out_element<X>(x, r8, i);
                 const float y = sum == 0.0f ? 0.0f : J.o[n][i * 2 + e] * f;
                 if (d < A.c.dim) out[d] = from_float<Q>(y);
-                if (d < A.c.dim && y != y && sum == sum) bad |= 1u << hd;
+                if (!X::E8 && d < A.c.dim && y != y && sum == sum) bad |= 1u << hd;
             }
             if (x == 0 && r8 == 0) {
                 const int64_t row = (int64_t)b * A.q.heads + h0 + hd;
@@ -963,18 +1083,18 @@ template <class X> __device__ __forceinline__ void write_joined(const DecodeArgs
                 A.lse2[row] = y;
             }
         }
+    if (X::E8) return 0;
     bad = __reduce_or_sync(FULL_MASK, bad);
-    while (bad) {
-        const int hd = __ffs(bad) - 1;
-        bad &= bad - 1;
-        float y = 0.0f;
+    if (bad) {
 #pragma unroll
         for (int n = 0; n < X::NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                if (n * 8 + e == (hd & 9)) y = J.m[n][e] + log2f(J.l[n][e]);
-        decode_repair<X>(A, b, h0 + hd, x, __shfl_sync(FULL_MASK, y, (hd & 7) >> 1));
+            for (int e = 0; e < 2; ++e) {
+                const float y = __shfl_sync(FULL_MASK, J.m[n][e] + log2f(J.l[n][e]), (lane & 7) >> 1);
+                if (lane >> 3 == n && (lane & 1) == e) *norm = y;
+            }
     }
+    return bad;
 }
 
 template <class X>
@@ -1079,11 +1199,15 @@ __global__ void __launch_bounds__(KLPM_DECODE_WARPS * 32, X::CTAS) decode_kernel
 }
 
 // Rows that were cut into parts, and rows with nothing to attend to.  An item is 16 elements of a unit, for WPR warps: a CTA where few rows
-// have many parts each, a warp where many rows have few.
+// have many parts each, a warp where many rows have few.  Four CTAs on an SM where the sums of 8 heads leave room (64 sequences, 2 cache heads: 18.4 us with four, 20.0
+// with three); with 16 heads registers count for more (100 sequences: 40.0 us with two CTAs, 41.0 with three).
 template <class X, int WPR>
-__global__ void __launch_bounds__(WPR == 1 ? 256 : WPR * 32) decode_join_kernel(const __grid_constant__ DecodeArgs A) {
+__global__ void __launch_bounds__(WPR == 1 ? 256 : WPR * 32, WPR <= 8 && X::NT == 1 ? 4 : 1) decode_join_kernel(const __grid_constant__ DecodeArgs A) {
     using Q = typename Elem<X::TQ>::T;
     __shared__ float4 s_all[WPR > 1 ? WPR * X::NT * 2 * 32 : 1];
+    __shared__ RepairShared<WPR> s_repair;
+    __shared__ float s_norm[32];
+    __shared__ unsigned s_bad;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -1097,12 +1221,18 @@ __global__ void __launch_bounds__(WPR == 1 ? 256 : WPR * 32) decode_join_kernel(
     const long long R = t0 * A.units + u * tiles, E = R + tiles;
     const int32_t w0 = (int32_t)(R / span), parts = tiles > 0 ? (int32_t)((E - 1) / span) - w0 + 1 : 0;
     if (parts == 1) {                                        // decode_kernel has written it; is there anything to repair?
-        if (WPR > 1 && warp) return;
-        const int d = out_element<X>(x, lane & 7, (lane >> 3) & 1);
-        for (int32_t hd = 0; hd < heads; ++hd) {
-            const Q* out = reinterpret_cast<const Q*>(A.out.p + b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
-            const float lse2 = A.lse2[(int64_t)b * A.q.heads + h0 + hd], y = d < A.c.dim ? to_float(out[d]) : 0.0f;
-            if (__any_sync(FULL_MASK, y != y) && lse2 == lse2) decode_repair<X>(A, b, h0 + hd, x, lse2);
+        if constexpr (!X::E8) {
+            if (WPR > 1 && warp) return;
+            const int d = out_element<X>(x, lane & 7, (lane >> 3) & 1);
+            unsigned bad = 0;
+            const float norm = lane < heads ? A.lse2[(int64_t)b * A.q.heads + h0 + lane] : 0.0f;
+            for (int32_t hd = 0; hd < heads; ++hd) {
+                const Q* out = reinterpret_cast<const Q*>(A.out.p + b * A.out.sr + (int64_t)(h0 + hd) * A.out.sh);
+                const float y = d < A.c.dim ? to_float(out[d]) : 0.0f;
+                if (__any_sync(FULL_MASK, y != y)) bad |= 1u << hd;
+            }
+            bad &= __ballot_sync(FULL_MASK, norm == norm);
+            if (bad) decode_repair<X, 1>(A, b, h0, bad, norm, x, nullptr);
         }
         return;
     }
@@ -1113,10 +1243,21 @@ __global__ void __launch_bounds__(WPR == 1 ? 256 : WPR * 32) decode_join_kernel(
     if constexpr (WPR > 1) {
         J.put(s_all + warp * X::NT * 2 * 32);
         __syncthreads();
-        if (warp) return;
-        J.take(s_all, WPR);
+        if (warp == 0) J.take(s_all, WPR);
     }
-    write_joined<X>(A, J, b, h0, heads, x);
+    float norm = 0.0f;
+    unsigned bad = 0;
+    if (WPR == 1 || warp == 0) bad = write_joined<X>(A, J, b, h0, heads, x, &norm);
+    if constexpr (!X::E8) {
+        if constexpr (WPR > 1) {
+            if (warp == 0) s_norm[lane] = norm;
+            if (__syncthreads_or(bad)) {
+                if (threadIdx.x == 0) s_bad = bad;
+                __syncthreads();
+                decode_repair<X, WPR>(A, b, h0, s_bad, s_norm[lane], x, &s_repair);
+            }
+        } else if (bad) decode_repair<X, 1>(A, b, h0, bad, norm, x, nullptr);
+    }
 }
 
 // Small calls: a cluster of CTAs per row (sequence, unit), its tiles dealt out to all of the cluster's warps, whose results are joined through
@@ -1133,6 +1274,9 @@ __global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_k
     __shared__ unsigned s_there[KLPM_ROW_WARPS][8];
     __shared__ float4 s_all[KLPM_ROW_WARPS * NT * 2 * 32];
     __shared__ float s_lse2[X::HEADS];
+    __shared__ RepairShared<KLPM_ROW_WARPS> s_repair;
+    __shared__ float s_norm[KLPM_ROW_WARPS][32];
+    __shared__ unsigned s_bad[KLPM_ROW_WARPS];
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int32_t ctas = 1 << lg, rank = blockIdx.x & (ctas - 1), row = blockIdx.x >> lg;
@@ -1174,8 +1318,22 @@ __global__ void __launch_bounds__(KLPM_ROW_WARPS * 32, X::CTAS / 2) decode_row_k
             __syncthreads();
             if (mine_of == 0) J.take(s_all + warp * NT * 2 * 32, share);
         }
-        if (x < X::KS && mine_of == 0) write_joined<X>(A, J, c.b, h0, heads, x);
-        if (share > 1) __syncthreads();
+        float norm = 0.0f;
+        unsigned bad = 0;
+        if (x < X::KS && mine_of == 0) bad = write_joined<X>(A, J, c.b, h0, heads, x, &norm);
+        if constexpr (X::E8) {
+            if (share > 1) __syncthreads();
+        } else {
+            if (share == 1) {
+                if (bad) decode_repair<X, 1>(A, c.b, h0, bad, norm, x, nullptr);
+            } else if (__syncthreads_or(bad)) {               // all of the CTA's warps, for one of its output tiles after the other
+                s_norm[warp][lane] = norm;
+                if (lane == 0) s_bad[warp] = bad;
+                __syncthreads();
+                for (int w = 0; w < KLPM_ROW_WARPS; w += share)
+                    if (s_bad[w]) decode_repair<X, KLPM_ROW_WARPS>(A, c.b, h0, s_bad[w], s_norm[w][lane], x0 + (w >> lg_share), &s_repair);
+            }
+        }
     }
     if (A.weight) {                                           // (one unit per cache head)
         for (int hd = warp; hd < heads; hd += KLPM_ROW_WARPS) {
