@@ -52,7 +52,8 @@ typedef struct {
 } kv_cache;
 
 /* Rows of heads outside the cache: element d of head h of row r is data[r * stride[0] + h * stride[1] + d] (strides in elements;
- * the number of rows is the call's).  Any alignment that the type itself needs. */
+ * the number of rows is the call's).  Any alignment that the type itself needs.  Rows that are written (out, q_out, and likewise those of
+ * d_weight in kv_decode and d_new_weight) lie apart from one another: RT_ERR_INVALID where their strides let two share memory. */
 typedef struct {
     void* data;
     int32_t dtype;     /* KV_F32, KV_BF16 or KV_F16 */

@@ -78,6 +78,24 @@ rt_status check_rows(const kv_rows* r, int32_t n) {
     return RT_OK;
 }
 
+// Whether rows of len elements at i * s0 + j * s1, i < n0, j < n1, lie apart: nothing two threads write may be the same.  Two of them overlap where some
+// |i s0 - j s1| < len; usually one dimension lies within the other's stride.
+bool rows_apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t len) {
+    using wide = __int128;
+    if (len < 1 || n0 < 1 || n1 < 1) return true;
+    wide a = s0 < 0 ? -(wide)s0 : s0, b = s1 < 0 ? -(wide)s1 : s1;
+    if (n0 > 1 && a < len) return false;
+    if (n1 > 1 && b < len) return false;
+    if (n0 == 1 || n1 == 1) return true;
+    if (a > b) { const wide t = a; a = b; b = t; const int64_t n = n0; n0 = n1; n1 = n; }            // a: the smaller stride, of n0 rows
+    if (b >= (wide)(n0 - 1) * a + len) return true;
+    for (int64_t j = 1; j < n1 && j * b < (wide)(n0 - 1) * a + len; ++j) {
+        const wide i = j * b / a, over = j * b - i * a;       // the rows of the other dimension on either side
+        if ((i < n0 && over < len) || (i + 1 < n0 && a - over < len)) return false;
+    }
+    return true;
+}
+
 // The cache as kernels see it: strides in bytes, dimensions of one entry with stride 0.
 struct CacheDev {
     char *k, *v;
@@ -1839,6 +1857,7 @@ rt_status kv_rope_append(const kv_cache* cache, const kv_rope* rope, const int32
     if (k->n_heads != cache->n_heads || v->n_heads != cache->n_heads || v->dtype != k->dtype) return RT_ERR_INVALID;
     if (q && (q->dtype != k->dtype || q_out->dtype != k->dtype || q->n_heads != q_out->n_heads)) return RT_ERR_INVALID;
     if (q && q->data == q_out->data && (q->stride[0] != q_out->stride[0] || q->stride[1] != q_out->stride[1])) return RT_ERR_INVALID;
+    if (q && !rows_apart(n, q_out->stride[0], q_out->n_heads, q_out->stride[1], cache->head_dim)) return RT_ERR_INVALID;
     if (k->dtype != KV_F32 && cache->dtype != KV_E4M3 && cache->dtype != k->dtype) return RT_ERR_INVALID;
     if (rope) {
         if (!rope->d_turns || rope->rot_dim < 2 || rope->rot_dim % 2 || rope->rot_dim > cache->head_dim) return RT_ERR_INVALID;
@@ -1915,7 +1934,9 @@ rt_status kv_decode(const kv_cache* cache, const kv_rows* q, const kv_rows* out,
     if (n_seqs > 65535 || (int64_t)max_pages * cache->page_size > KLPM_MAX_TOKENS) return RT_ERR_TOO_LARGE;
     if (n_seqs > 0 && (!d_lengths || (max_pages > 0 && !d_page_table))) return RT_ERR_INVALID;
     if (table_stride < max_pages && n_seqs > 1) return RT_ERR_INVALID;
-    if (d_weight && !weight_stride) return RT_ERR_INVALID;
+    if (!rows_apart(n_seqs, out->stride[0], out->n_heads, out->stride[1], cache->head_dim)) return RT_ERR_INVALID;
+    if (d_weight && (!weight_stride || !rows_apart(n_seqs, weight_stride[0], cache->n_heads, weight_stride[1], (int64_t)max_pages * cache->page_size)))
+        return RT_ERR_INVALID;
     const int64_t need = kv_decode_workspace(cache, n_seqs, q->n_heads, max_pages, d_weight != nullptr);
     if (need < 0) return (rt_status)need;
     if (need > 0 && (!d_workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(d_workspace) % 256)) return RT_ERR_INVALID;
@@ -1946,6 +1967,7 @@ rt_status kv_evict(const kv_cache* cache, const float* d_weight, const int64_t* 
     if (keep > KLPM_MAX_TOKENS || new_weight_len > KLPM_MAX_TOKENS) return RT_ERR_TOO_LARGE;
     if (n_seqs > 1 && (table_stride < max_pages || new_stride < new_pages)) return RT_ERR_INVALID;
     if (!weight_stride || !new_weight_stride) return RT_ERR_INVALID;
+    if (!rows_apart(n_seqs, new_weight_stride[0], cache->n_heads, new_weight_stride[1], new_weight_len)) return RT_ERR_INVALID;
     if (n_seqs > 0 && (!d_lengths || !d_new_table || !d_index || !d_new_weight || !d_new_lengths)) return RT_ERR_INVALID;
     if (n_seqs > 0 && max_pages > 0 && (!d_page_table || !d_weight || d_weight == d_new_weight)) return RT_ERR_INVALID;
     if (n_seqs == 0) return RT_OK;

@@ -139,3 +139,26 @@ def test_a_nan_value_does_not_make_a_call_slow(tc, seqs, length):
     assert out[0].isnan().all() and out[1:].isfinite().all()
     print("%s %d x %d: %.1f us, with a NaN %.1f us" % (tc, seqs, length, clean * 1e3, bad * 1e3))
     assert bad < 25 * clean
+
+
+def test_outputs_whose_rows_lie_apart_in_any_order():
+    """Heads before sequences, and rows that fill one another's gaps: what is refused is memory shared by two rows, not an unusual layout."""
+    g = gen(23)
+    lens = [90, 33, 7]
+    table, pages = tables(g, lens, 16)
+    c = make_cache(g, pages, 16, 2, 64, BF)
+    q = torch.randn(3, 2, 64, generator=g, device="cuda").to(BF)
+    lengths = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    want, want_w = torch.empty_like(q), torch.zeros(3, 2, table.shape[1] * 16, device="cuda")
+    K().kv_decode(c, q, table, lengths, want, weight=want_w)
+    width = want_w.shape[2]
+    for s0, s1 in ((64, 3 * 64), (2 * 64, 3 * 64), (3 * 64, 64), (70, 300)):
+        room = torch.full((600,), 9.0, dtype=BF, device="cuda")
+        out = room.as_strided((3, 2, 64), (s0, s1, 1))
+        w = torch.zeros(9 * width, device="cuda").as_strided((3, 2, width), (s0 * width // 64, s1 * width // 64, 1))
+        turned = room.clone().as_strided((3, 2, 64), (s0, s1, 1))
+        K().kv_decode(c, q, table, lengths, out, weight=w)
+        K().kv_rope_append(c, q, q, torch.full((3,), -1, dtype=torch.int32, device="cuda"), q=q, q_out=turned)
+        assert torch.equal(out, want) and torch.equal(w, want_w) and torch.equal(turned, q)
+        out.fill_(9.0)
+        assert (room == 9).all()

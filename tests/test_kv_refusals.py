@@ -152,3 +152,16 @@ def test_the_binding_refuses_numbers_that_do_not_fit(K):
         with pytest.raises(ValueError):
             K._count(x, "window")
     assert K._count((1 << 31) - 1, "window") == (1 << 31) - 1
+
+
+def test_outputs_whose_rows_overlap_are_refused(K):
+    """Expanded outputs and others that share memory between rows: two rows would be written (or added to) at the same time."""
+    c = cache(K)
+    for stride in [(0, 64), (1024, 0), (1024, 63), (64, 64), (128, 64), (255, 64), (-128, 64), (96, 64), (0, 0), (64, 128), (1 << 62, 32)]:
+        assert decode(K, c, out=rows(K, 4, data=2 * P, stride=stride)) == K.RT_ERR_INVALID, stride
+        assert append(K, c, q=rows(K, 4), q_out=rows(K, 4, data=2 * P, stride=stride)) == K.RT_ERR_INVALID, stride
+        assert append(K, c, q=rows(K, 4, stride=stride), q_out=rows(K, 4, stride=stride)) == K.RT_ERR_INVALID, stride
+    for ws in [(0, 128), (256, 0), (255, 128), (128, 128), (256, 127), (0, 0), (127, 1 << 40)]:         # rows of 8 pages of 16 tokens
+        assert decode(K, c, weight=P, ws=ws) == K.RT_ERR_INVALID, ws
+    for nws in [(0, 128), (256, 0), (200, 128), (128, 128), (0, 0)]:
+        assert evict(K, c, nws=nws) == K.RT_ERR_INVALID, nws
