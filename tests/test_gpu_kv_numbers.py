@@ -1,5 +1,6 @@
 """Numbers at the ends of their types in the KV-cache operators.  The plain implementations and the bounds are those of test_gpu_kv.py."""
 import math
+from fractions import Fraction
 
 import pytest
 import torch
@@ -162,3 +163,23 @@ def test_outputs_whose_rows_lie_apart_in_any_order():
         assert torch.equal(out, want) and torch.equal(w, want_w) and torch.equal(turned, q)
         out.fill_(9.0)
         assert (room == 9).all()
+
+
+@pytest.mark.parametrize("rot", [16, 128])
+def test_far_positions_against_exact_turns(rot):
+    """Positions up to the ends of 31 bits, whole turns taken off in rational arithmetic.  The kernel's product in 64 bits is off by half a step, at 2^31 positions
+    of 1 / (2 pi) turns 2^-25 of a turn, its rest in 32 bits by 2^-26 more, and sine and cosine by 2 ulp: the angle by less than 2^-24 of a turn, 2 pi
+    2^-24 or 6.3 u; two products and a sum, with the factors' errors, 6 u."""
+    rope = K().kv_rope_table(rot, theta=10_000.0, device="cuda")
+    positions = [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 12345, 1_500_000_001, 987_654_321, -77, 1 << 20, 0]
+    n, turns = len(positions), [Fraction(x) for x in rope.turns.tolist()]
+    exact = torch.tensor([[float((p * f) % 1) for f in turns] for p in positions], dtype=torch.float64, device="cuda")[:, None] * (2 * math.pi)
+    q = torch.randn(n, 3, rot, generator=gen(41), device="cuda")
+    c = make_cache(gen(1), 4, 4, 1, rot, BF)
+    got = torch.empty_like(q)
+    K().kv_rope_append(c, q[:, :1], q[:, :1], torch.full((n,), -1, dtype=torch.int32, device="cuda"),
+                       positions=torch.tensor(positions, dtype=torch.int32, device="cuda"), rope=rope, q=q, q_out=got)
+    a, b = q.double()[..., :rot // 2], q.double()[..., rot // 2:]
+    want = torch.cat([a * exact.cos() - b * exact.sin(), a * exact.sin() + b * exact.cos()], -1)
+    size = (a.abs() + b.abs()).repeat(1, 1, 2)
+    assert ((got.double() - want).abs() <= 13 * U * size).all()
