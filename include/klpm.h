@@ -123,7 +123,10 @@ rt_status rt_match_batch_ex(rt_tree* tree, const int32_t* d_q_tokens, const int6
  * d_match_len are what rt_match_batch wrote; insertions since then change nothing, evictions and rt_rollback void them (the row then holds
  * other indices of the pool, or -1).  Two prompts that share a prefix get the same indices for it, and a token keeps its index until it is
  * evicted: with the keys and values of token-pool index s in slot s of a cache, a row is that prompt's page table with pages of one token
- * (klpm_kv.h).  A node or length that is not one leaves a row of -1.  RT_ERR_TOO_LARGE if max_pool_tokens is above 2^31 - 1. */
+ * (klpm_kv.h).  The pool is append-only, with up to 6 tokens of padding per prompt, and short of rt_rollback an evicted token's index is not
+ * handed out again: a cache addressed this way has a slot for every token that was ever stored and for the padding (max_pool_tokens), and
+ * evictions under budget_tokens free none of them.  An engine that is to hold no more than its budget maps indices to slots of its own.
+ * A node or length that is not one leaves a row of -1.  RT_ERR_TOO_LARGE if max_pool_tokens is above 2^31 - 1. */
 rt_status rt_prefix_slots(const rt_tree* tree, const int32_t* d_term_node, const int32_t* d_match_len, int32_t nq,
                           int32_t* d_slots, int64_t row_stride, int32_t max_len, void* stream);
 

@@ -16,7 +16,8 @@
  * nothing.  Calls on different streams may overlap on the GPU unless one writes what the other uses; a workspace belongs to one
  * call at a time (two captured graphs that may run at the same time need a workspace each).
  *
- * Sums, softmax statistics and rotations are held in 32-bit floating point (rotation angles in 64) and rounded once, when stored.
+ * Sums, softmax statistics and rotations are held in 32-bit floating point (rotation angles in 64) and rounded once, when stored; kv_decode
+ * rounds probabilities, and bf16 queries next to an 8-bit cache, on the way (see there).
  */
 #ifndef KLPM_KV_H_
 #define KLPM_KV_H_
@@ -78,7 +79,9 @@ enum { KV_ROPE_PLAIN = 0, KV_ROPE_LINEAR = 1, KV_ROPE_NTK = 2, KV_ROPE_YARN = 3 
  *   KV_ROPE_LINEAR  positions divided by scale
  *   KV_ROPE_NTK     theta * scale^(rot_dim / (rot_dim - 2)): the slowest pair is slowed by scale, the fastest not at all
  *   KV_ROPE_YARN    pairs that turn more than beta_fast times within original_len are kept, those that turn less than beta_slow times
- *                   are divided by scale, linear in between (YaRN, arXiv 2309.00071); *factor becomes 0.1 ln(scale) + 1
+ *                   are divided by scale, linear in the number of turns in between (YaRN, arXiv 2309.00071); *factor becomes 0.1 ln(scale) + 1.
+ *                   Programs that ramp over the pair's number instead (between the two pairs' numbers, often rounded) have other frequencies:
+ *                   a model made with those needs a d_turns of its own, which the caller may fill as it likes
  * *factor (host, nullable) is 1 otherwise. */
 rt_status kv_rope_table(double* d_turns, int32_t rot_dim, double theta, int32_t scaling, double scale, double original_len,
                         double beta_fast, double beta_slow, float* factor, void* stream);
@@ -86,7 +89,7 @@ rt_status kv_rope_table(double* d_turns, int32_t rot_dim, double theta, int32_t 
 /* For i < n: rotate head rows q[i] (nullable) into q_out[i] and k[i] by d_positions[i] (rope NULL: no rotation, d_positions may be
  * NULL), and store k[i], v[i] at slot d_slots[i] of the cache (divided by the scale and rounded to the nearest; 8-bit values saturate at
  * +-448, NaN stays NaN).  q, q_out, k and v have one dtype; it is the cache's, or the cache's is KV_E4M3, or it is KV_F32.
- * q_out may be q itself; otherwise they must not overlap.  A slot outside [0, n_pages * page_size) (a padded row) is not stored; its
+ * q_out may be q itself; otherwise they must not overlap, nor may the cache's k and v.  A slot outside [0, n_pages * page_size) (a padded row) is not stored; its
  * query is rotated all the same.  No slot may occur twice in a call (each element of such a slot is one of the two rows'). */
 rt_status kv_rope_append(const kv_cache* cache, const kv_rope* rope, const int32_t* d_positions, const int32_t* d_slots, int32_t n,
                          const kv_rows* q, const kv_rows* q_out, const kv_rows* k, const kv_rows* v, void* stream);
@@ -106,10 +109,17 @@ int64_t kv_decode_workspace(const kv_cache* cache, int32_t n_seqs, int32_t n_q_h
  *             their softmax weights of token t (max_pages * page_size entries per row; those of masked tokens stay as they are)
  *   q, out    one dtype: the cache's, or either 16-bit type if the cache is KV_E4M3.  They must not overlap.
  *   n_seqs    at most 65,535 (so for kv_evict)
- *   d_workspace  kv_decode_workspace bytes, aligned to 256; its contents before and after the call mean nothing
- * The result is the same for every call with the same arguments (no atomics on floating-point values).  Sums are formed before they are divided by
- * the softmax's sum: the number of tokens times the largest value, times 2^15 for f16 and 8-bit caches, has to stay within 32-bit floating
- * point.  Infinite and NaN keys or values of tokens that are attended to come out as the formula says. */
+ *   d_workspace  kv_decode_workspace bytes, aligned to 256; its contents before and after the call mean nothing.  With d_weight it holds
+ *             n_seqs * n_q_heads * max_pages * page_size scores of 4 bytes, whatever d_lengths says (128 sequences, 32 heads, tables for 131,072
+ *             tokens: 2.1 GB): tables no wider than the longest sequence save most of it
+ * The result is the same for every call with the same arguments (no atomics on floating-point values).
+ * Roundings on the way: a probability enters the sum of values as the sum of two 16-bit numbers, off by 2^-16 of it at most next to a bf16 cache, else by
+ * 2^-22 of it, or 2^-39 of the row's largest if that is more; a bf16 query next to an 8-bit cache has elements off by 2^-39 of the head's largest at most.
+ * Range: q . k before it is scaled (of a bf16 query next to an 8-bit cache: scale * k_scale times its largest element) has to stay within 32-bit floating
+ * point.  So do sums of values, which are formed before they are divided by the softmax's sum: the number of tokens times the largest value, times 2^15 for f16 and 8-bit caches.
+ * Infinite and NaN keys or values of tokens that are attended to come out as the formula says: an infinite value makes the output infinite however small
+ * its probability, and with the other infinity, or if it is NaN, NaN; a token whose score is -inf takes no part, whatever its value.  They cost
+ * time, see decode_repair in csrc/klpm_kv.cu: a few times a call's, some hundred times only where a token with a score of -inf has such a value. */
 rt_status kv_decode(const kv_cache* cache, const kv_rows* q, const kv_rows* out, int32_t n_seqs, const int32_t* d_page_table,
                     int64_t table_stride, int32_t max_pages, const int32_t* d_lengths, float scale, int32_t window, float* d_lse,
                     float* d_weight, const int64_t* weight_stride, void* d_workspace, int64_t workspace_bytes, void* stream);

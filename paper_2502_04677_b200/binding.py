@@ -218,7 +218,7 @@ def rt_match_batch_ex(tree: Tree, q_tokens: torch.Tensor, q_offsets: torch.Tenso
 
 def rt_prefix_slots(tree: Tree, term_node: torch.Tensor, match_len: torch.Tensor, slots: torch.Tensor) -> None:
     """slots (int32[nq, max_len]) receives the token-pool indices of every query's match, -1 behind its end: the page
-    table of the cached prefixes with pages of one token (see include/klpm.h)."""
+    table of the cached prefixes with pages of one token (see include/klpm.h, also for what that asks of the cache's size)."""
     nq = match_len.numel()
     if term_node.numel() != nq or slots.dim() != 2 or slots.shape[0] != nq:
         raise ValueError("term_node, match_len and the rows of slots must be one per query")
@@ -479,7 +479,7 @@ class Rope:
 def kv_rope_table(rot_dim: int, theta: float = 10_000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
                   original_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda") -> Rope:
     """The frequencies of rotary positions over the first rot_dim elements of a head, scaled for contexts `factor` times as long as
-    original_len: scaling "none", "linear", "ntk" or "yarn" (see include/klpm_kv.h)."""
+    original_len: scaling "none", "linear", "ntk" or "yarn" (see include/klpm_kv.h, also for checkpoints whose YaRN ramps otherwise)."""
     _count(rot_dim, "rot_dim")
     if scaling not in ROPE_SCALINGS:
         raise ValueError("scaling must be one of %s" % ", ".join(sorted(ROPE_SCALINGS)))
@@ -573,7 +573,8 @@ def kv_decode(cache: KvCache, q: torch.Tensor, page_table: torch.Tensor, lengths
     """Attention of one new token per sequence: q, out [n_seqs, q_heads, head_dim], page_table int32[n_seqs, max_pages], lengths
     int32[n_seqs].  scale defaults to head_dim ** -0.5.  lse float32[n_seqs, q_heads] receives the logarithm of the softmax's sum;
     weight float32[n_seqs, n_heads, max_pages * page_size] is increased by what every cached token received.  Without a
-    workspace (kv_decode_workspace) the call takes one from torch's allocator."""
+    workspace (kv_decode_workspace) the call takes one from torch's allocator; with weight that is 4 bytes per sequence, query head and token of the
+    table's width, whatever the lengths are."""
     n = lengths.numel()
     table, stride, max_pages = _pages(page_table, cache, n, "page_table")
     rq = _rows(q, cache, n, "q")
