@@ -295,8 +295,8 @@ template <int TX, int TC> void launch_append(const AppendArgs& A, bool vec, dim3
 // The floor is one read of the cache's rows (512 B per token and cache head at 128 elements of 16 bits, against a few flops per
 // byte), so everything is laid out for loads in flight:
 //   - Up to 16 query heads of a cache head (8 where heads have more than 128 elements: the sums are in registers) go through the tensor cores together
-//     (mma.sync, 16 x 8 x 16): a tile of keys is read once for all of them.  More query heads are units of their own, which read it again.  Tokens, then elements of the values, take the 16 rows of the operand that comes from shared memory, 8 heads the
-//     8 columns.  tcgen05 has nothing to give here: its tiles would hold 128 rows for a few flops per byte that is read anyway.
+//     (mma.sync, 16 x 8 x 16): a tile of keys is read once for all of them.  More query heads are units of their own, which read it again.  Tokens,
+//     then elements of the values, take the 16 rows of the operand that comes from shared memory, 8 heads the 8 columns.  tcgen05 has nothing to give here: its tiles would hold 128 rows for a few flops per byte that is read anyway.
 //   - A warp works alone: its half tiles (keys, then values, of 16 or 32 tokens) come through a ring of its own in shared
 //     memory (cp.async, 16 bytes a lane), with its own m and sums.  No barrier in the loop.  The warps of an SM hide what the
 //     dependent steps of one take.  Up to 128 elements and 8 query heads there are 16 of them, with half tiles of 4 KB (2 KB: 64 elements in 8 bits) of which
@@ -306,8 +306,9 @@ template <int TX, int TC> void launch_append(const AppendArgs& A, bool vec, dim3
 //     A unit is a cache head and up to 8 NT of its query heads.
 //   - Probabilities enter the second product as the sum of two 16-bit numbers (off by 2^-16 of each at most with bf16, 2^-22 with f16, there nothing below
 //     2^-39 of the row's largest), whose products go to the same sums; what divides them is summed before that.  One bf16 number would add as much error as the
-//     output's own rounding has; a third would cost a third more products for what that rounding hides.  f16 probabilities are scaled by 2^15 so that small ones keep their bits.  A bf16 query next to an 8-bit cache
-//     becomes f16, times a power of two per head that brings its largest element next to 2^15: exact down to 2^-29 of that, nothing below 2^-39 of it.
+//     output's own rounding has; a third would cost a third more products for what that rounding hides.  f16 probabilities are scaled
+//     by 2^15 so that small ones keep their bits.  A bf16 query next to an 8-bit cache becomes f16, times a power of two per head that brings its largest
+//     element next to 2^15: exact down to 2^-29 of that, nothing below 2^-39 of it.
 // Measured (a graph of calls; MB are those that have to be read): 128 sequences of up to 16,384 tokens, 4.28 GB in 650 us, 6.6 TB/s, what a plain
 // copy reaches; 33 of up to 8,191, 557 MB in 99 us, 10 us of which are start and join, with weights 115 us; 2 of 131,072 in 8 bits, 268 MB
 // in 60 us: the conversions to f16 take as many instructions as everything else.
